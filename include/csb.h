@@ -1,6 +1,7 @@
 /*
- * libcsb -- compressed-structured-block (CSB) sparse products and the fused
- * LSTM / GRU time loop on one NVIDIA B200 (sm_100a).
+ * libcsb -- compressed-structured-block (CSB) sparse products, the fused
+ * LSTM / GRU time loop, and what serves recurrent language models beside them
+ * (low-rank adapters, the gated delta rule) on one NVIDIA B200 (sm_100a).
  *
  * The operations follow "CSB-RNN" (arXiv 2005.05758):
  *   - the CSB matrix and its storage format: Section 3.1.1;
@@ -47,9 +48,11 @@ typedef enum csb_status {
 } csb_status;
 
 enum { CSB_F32 = 0, CSB_F16 = 1,            /* storage type of the packed values */
-       CSB_Q16 = 2 };                       /* 16-bit fixed point; handles made by csb_encode_q16 only */
+       CSB_Q16 = 2,                         /* 16-bit fixed point; handles made by csb_encode_q16 only */
+       CSB_BF16 = 3 };                      /* of csb_spmm_adapters' adapters and csb_gated_delta_*'s tensors only */
 enum { CSB_FLAG_ASYNC = 1u,                 /* recurrent calls: do not wait for the status word */
-       CSB_FLAG_HOST_IO = 2u };             /* recurrent calls: sequence and state pointers are host memory */
+       CSB_FLAG_HOST_IO = 2u,               /* recurrent calls: sequence and state pointers are host memory */
+       CSB_FLAG_NORMALIZE = 4u };           /* csb_gated_delta_*: queries and keys are normalised by the call */
 
 typedef struct csb_matrix csb_matrix_t;     /* opaque: canonical arrays + device layout + schedule */
 
@@ -334,6 +337,81 @@ int csb_ligru_forward(int n_layers, const csb_matrix_t* const* W, const float* c
                       const float* h0, float* y, float* hT, unsigned flags, void* stream);
 int csb_gru_reset_before_forward(int n_layers, const csb_matrix_t* const* W, const float* const* bias, const float* x, int64_t T,
                                  int B, const float* h0, float* y, float* hT, unsigned flags, void* stream);
+
+/*
+ * csb_spmm_adapters -- csb_spmm with a low-rank adapter of its own for every request beside the shared matrix (the paper
+ * has no counterpart; it is how one pruned projection serves many fine-tuned models at once):
+ *   Y[b, :] = A . X[b, :] + s_a * up_a . (down_a . X[b, :]),   a = which[b].
+ *   A, X, ldx, batch, Y, ldy   as for csb_spmm.
+ *   dtype   type of the adapters: CSB_F32, CSB_F16 or CSB_BF16.
+ *   count, rank   adapters, and the rank that their tensors have room for (1..256).
+ *   down    device, [count, rank, cols], contiguous;  up  device, [count, rows, rank], contiguous.
+ *   which   device, int32 [batch]: the adapter of each request; one outside 0 .. count - 1 means none.
+ *   ranks   device, int32 [count] or NULL: the rank each adapter really has (clipped to 0 .. rank); what down and up
+ *           hold beyond it is not read.   scales  device, float32 [count] or NULL (ones).
+ *   workspace   device, csb_adapters_workspace_bytes(A, batch, rank) bytes of scratch, caller-owned, 4-byte aligned: two
+ *           calls that may overlap on the GPU, or two captured graphs, need one each.
+ * The requests may name their adapters in any order.  fp32 sums in a fixed order (bit-reproducible); the inputs are not rounded
+ * (each is taken as two tf32 halves, 22 bits).  A request's outputs depend on no other request's input and on no other adapter.
+ * A non-finite input gives non-finite values in its own request's outputs.
+ * Three or more launches with programmatic stream serialization, asynchronous on `stream`; csb_spmm's rules on
+ * overlapping calls and on the first call with a handle hold.  The current device must be the matrix's.
+ * Errors: INVALID_ARG (null, sizes, workspace too small, another device current), SHAPE, DTYPE, UNSUPPORTED (rank above 256,
+ * host-only or fixed-point handle), and those of csb_spmm.
+ */
+int64_t csb_adapters_workspace_bytes(const csb_matrix_t* A, int batch, int rank);
+int csb_spmm_adapters(const csb_matrix_t* A, const float* X, int64_t ldx, int batch, float* Y, int64_t ldy, int dtype, int count, int rank,
+                      const void* down, const void* up, const int32_t* which, const int32_t* ranks, const float* scales,
+                      void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The gated delta rule: a linear recurrent cell whose hidden state is a matrix (the paper has no counterpart; it is the
+ * recurrence of language models that keep a state of fixed size instead of a cache).  Per value head, token by token:
+ *   S <- e^g S;   S <- S + k (beta (v - S^T k))^T;   o = scale S^T q.
+ *
+ * csb_gated_delta_forward -- whole sequences of different lengths, packed behind one another (prompts).
+ * csb_gated_delta_step    -- one token of each of `sequences` sequences (decoding); tokens = sequences.
+ *   shape   sizes and strides, see below.
+ *   q, k    device, [tokens, k_heads, k_dim];  v  device, [tokens, v_heads, v_dim], all of type shape->dtype; the heads of a
+ *           token are contiguous, tokens are ldq / ldk / ldv elements apart.  Value head h reads query and key head
+ *           h / (v_heads / k_heads).  With CSB_FLAG_NORMALIZE q and k are divided by sqrt(sum of squares + 1e-6).
+ *   g, beta device, float32 [tokens, v_heads], tokens ldg / ldb elements apart: log of the decay (<= 0 for a cell that forgets;
+ *           -inf drops the state) and strength of the write.
+ *   o       device, [tokens, v_heads, v_dim], type shape->dtype, tokens ldo elements apart; must not overlap the inputs.
+ *   state   device, float32 [slots, v_heads, k_dim, v_dim], contiguous: a pool of states, read and updated in place.  For
+ *           csb_gated_delta_forward it may be NULL: every sequence starts from zero, and no state is kept.
+ *   seq_begin  device, int32 [sequences + 1], ascending: sequence i has the tokens seq_begin[i] .. seq_begin[i + 1] - 1.
+ *           NULL with sequences = 1: one sequence of all tokens.
+ *           Tokens outside all of them are not touched.  (A value outside 0 .. tokens is clipped; where the values do not
+ *           ascend, the outputs are unspecified, but nothing outside the tensors is touched.)
+ *   slot    device, int32 [sequences] or NULL (sequence i has slot i): the slot of each sequence's state.  A sequence
+ *           whose slot is outside 0 .. slots - 1 (padding), or is named by an earlier sequence of the call already, is left
+ *           out: its outputs and states stay as they are.  So does the state of a sequence without tokens.
+ *   fresh   device, uint8 [sequences] or NULL: sequences whose byte is not zero start from a state of zeros, whatever the slot holds.
+ *   workspace  device, csb_gated_delta_workspace_bytes(shape) bytes of scratch, caller-owned, 16-byte aligned: two calls
+ *           that may overlap on the GPU, or two captured graphs, need one each.
+ * States, sums and decays are fp32; results are bit-reproducible.  The sizes are all the host looks at: no call
+ * allocates or synchronises, and all may be captured.  Calls that share slots must be ordered.  All pointers are on the
+ * current device.
+ * Errors: INVALID_ARG (null, sizes, scale, flags, workspace too small), SHAPE (heads that do not divide, short strides, a step
+ * with other than one token a sequence), DTYPE, UNSUPPORTED (k_dim above 256, v_dim above 65536, heads above 65535), CUDA.
+ */
+typedef struct csb_delta_shape {
+    int64_t tokens;              /* rows of q, k, v, g, beta and o                                 */
+    int64_t slots;               /* states in the pool                                             */
+    int32_t sequences;
+    int32_t k_heads, v_heads;    /* v_heads a multiple of k_heads                                  */
+    int32_t k_dim, v_dim;        /* of a head                                                      */
+    int32_t dtype;               /* CSB_F32, CSB_F16 or CSB_BF16                                   */
+    int64_t ldq, ldk, ldv, ldg, ldb, ldo;   /* elements from a token to the next                   */
+    float scale;                 /* of the outputs; 0 stands for 1 / sqrt(k_dim)                   */
+} csb_delta_shape_t;
+int64_t csb_gated_delta_workspace_bytes(const csb_delta_shape_t* shape);
+int csb_gated_delta_forward(const csb_delta_shape_t* shape, const void* q, const void* k, const void* v, const float* g, const float* beta, void* o,
+                            float* state, const int32_t* seq_begin, const int32_t* slot, const uint8_t* fresh, void* workspace, int64_t workspace_bytes,
+                            unsigned flags, void* stream);
+int csb_gated_delta_step(const csb_delta_shape_t* shape, const void* q, const void* k, const void* v, const float* g, const float* beta, void* o,
+                         float* state, const int32_t* slot, unsigned flags, void* stream);
 
 /*
  * csb_test_barrier_hook -- testing aid for the give-up path of the time loop's waits on other

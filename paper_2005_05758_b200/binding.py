@@ -25,8 +25,8 @@ except ImportError as e:
     raise ImportError("_csb_py is not built: run `python -m paper_2005_05758_b200.build`") from e
 
 CSB_F32, CSB_F16 = 0, 1
-CSB_FLAG_ASYNC, CSB_FLAG_HOST_IO = 1, 2
-CSB_Q16 = 2
+CSB_FLAG_ASYNC, CSB_FLAG_HOST_IO, CSB_FLAG_NORMALIZE = 1, 2, 4
+CSB_Q16, CSB_BF16 = 2, 3
 _DT = {"f32": CSB_F32, "f16": CSB_F16}
 
 
@@ -119,6 +119,7 @@ class CsbMatrix:
 
     def __init__(self, handle: int):
         self.handle = handle
+        self._shape = None
 
     def view(self) -> dict:
         v = csb_view_t()
@@ -144,6 +145,15 @@ class CsbMatrix:
         o = csb_info_t()
         _check(lib.csb_info(self.handle, C.byref(o)))
         return {k: getattr(o, k) for k, _ in csb_info_t._fields_}
+
+    @property
+    def shape(self) -> tuple:
+        """(rows, cols) of the matrix."""
+        if self._shape is None:
+            v = csb_view_t()
+            _check(lib.csb_view(self.handle, C.byref(v)))
+            self._shape = (v.rows, v.cols)
+        return self._shape
 
     def free(self) -> None:
         if self.handle:
@@ -308,6 +318,141 @@ def csb_ligru_forward(W: Sequence[CsbMatrix], bias, x, h0, y, hT, flags: int = 0
 
 def csb_gru_reset_before_forward(W: Sequence[CsbMatrix], bias, x, h0, y, hT, flags: int = 0, stream=None) -> None:
     _check(_csb_py.recurrent(_FN["csb_gru_reset_before_forward"], _GRU, W, None, bias, x, h0, None, y, hT, None, flags, _stream(stream)))
+
+
+class csb_delta_shape_t(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("slots", C.c_int64), ("sequences", C.c_int32), ("k_heads", C.c_int32), ("v_heads", C.c_int32),
+                ("k_dim", C.c_int32), ("v_dim", C.c_int32), ("dtype", C.c_int32), ("ldq", C.c_int64), ("ldk", C.c_int64), ("ldv", C.c_int64),
+                ("ldg", C.c_int64), ("ldb", C.c_int64), ("ldo", C.c_int64), ("scale", C.c_float)]
+
+
+lib.csb_adapters_workspace_bytes.argtypes = [_P, C.c_int, C.c_int]
+lib.csb_spmm_adapters.argtypes = [_P, _P, C.c_int64, C.c_int, _P, C.c_int64, C.c_int, C.c_int, C.c_int, _P, _P, _P, _P, _P, _P, C.c_int64, _P]
+lib.csb_gated_delta_workspace_bytes.argtypes = [C.POINTER(csb_delta_shape_t)]
+lib.csb_gated_delta_forward.argtypes = [C.POINTER(csb_delta_shape_t)] + [_P] * 11 + [C.c_int64, C.c_uint, _P]
+lib.csb_gated_delta_step.argtypes = [C.POINTER(csb_delta_shape_t)] + [_P] * 8 + [C.c_uint, _P]
+for _f in ("csb_adapters_workspace_bytes", "csb_gated_delta_workspace_bytes"):
+    getattr(lib, _f).restype = C.c_int64
+for _f in ("csb_spmm_adapters", "csb_gated_delta_forward", "csb_gated_delta_step"):
+    getattr(lib, _f).restype = C.c_int
+
+
+def _value_types():
+    import torch
+    return {torch.float32: CSB_F32, torch.float16: CSB_F16, torch.bfloat16: CSB_BF16}
+
+
+def _tensor(name, t, dtype, shape, where=None, inner=None):
+    """Refuses a tensor that the library would read wrongly: type, sizes (None: any), device, and that its last `inner`
+    dimensions lie behind one another (None: all of them)."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s: a torch tensor is expected, got %s" % (name, type(t).__name__))
+    if t.dtype != dtype:
+        raise TypeError("%s: %s is expected, got %s" % (name, dtype, t.dtype))
+    if t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
+        raise ValueError("%s: shape %s is expected, got %s" % (name, tuple("any" if w is None else w for w in shape), tuple(t.shape)))
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s: the current CUDA device is expected" % (name, t.device))
+    if where is not None and t.device != where:
+        raise ValueError("%s is on %s, the other tensors on %s" % (name, t.device, where))
+    step, strides = 1, t.stride()
+    for d in range(t.dim() - 1, (0 if inner is None else t.dim() - inner) - 1, -1):
+        if t.shape[d] != 1 and strides[d] != step and t.numel():
+            raise ValueError("%s: its last %d dimensions must be contiguous, strides are %s" % (name, t.dim() if inner is None else inner, strides))
+        step *= t.shape[d]
+    return t
+
+
+def _scratch(nbytes: int, given, device, stream):
+    """The caller's workspace, or one of torch's allocator that outlives the work queued on `stream`."""
+    import torch
+    if given is not None:
+        if not given.is_cuda or given.device != device or not given.is_contiguous():
+            raise ValueError("workspace: a contiguous tensor on %s is expected" % device)
+        return given, given.numel() * given.element_size()
+    buf = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+    if stream is not None:
+        st = _stream(stream)
+        if st != torch.cuda.current_stream(device).cuda_stream:
+            buf.record_stream(torch.cuda.ExternalStream(st or 0, device=device))
+    return buf, buf.numel()
+
+
+def csb_spmm_adapters(A: CsbMatrix, X, Y, down, up, which, ranks=None, scales=None, workspace=None, stream=None) -> None:
+    """Y[b] = A . X[b] + scales[a] * up[a] @ (down[a] @ X[b]) with a = which[b] (none where a is outside 0 .. len(down) - 1).
+
+    X float32 [batch, cols], Y float32 [batch, rows]; down [count, rank, cols] and up [count, rows, rank] of one type
+    (float32, float16 or bfloat16); which int32 [batch]; ranks int32 [count], scales float32 [count] (see csb.h)."""
+    import torch
+    types = _value_types()
+    if down.dtype not in types:
+        raise TypeError("down: float32, float16 or bfloat16 is expected, got %s" % down.dtype)
+    rows, cols = A.shape
+    _tensor("X", X, torch.float32, (None, cols), inner=1)
+    _tensor("down", down, down.dtype, (None, None, cols), X.device)
+    batch, (count, rank, _) = X.shape[0], down.shape
+    _tensor("Y", Y, torch.float32, (batch, rows), X.device, inner=1)
+    _tensor("up", up, down.dtype, (count, rows, rank), X.device)
+    _tensor("which", which, torch.int32, (batch,), X.device)
+    if ranks is not None:
+        _tensor("ranks", ranks, torch.int32, (count,), X.device)
+    if scales is not None:
+        _tensor("scales", scales, torch.float32, (count,), X.device)
+    buf, size = _scratch(int(lib.csb_adapters_workspace_bytes(A.handle, batch, rank)), workspace, X.device, stream)
+    _check(lib.csb_spmm_adapters(A.handle, _ptr(X), X.stride(0) if batch > 1 else cols, batch, _ptr(Y), Y.stride(0) if batch > 1 else rows,
+                                 types[down.dtype], count, rank, _ptr(down), _ptr(up), _ptr(which), _ptr(ranks), _ptr(scales), _ptr(buf), size,
+                                 _stream(stream)))
+
+
+def _delta_shape(q, k, v, g, beta, o, state, sequences, scale):
+    import torch
+    types = _value_types()
+    if q.dtype not in types:
+        raise TypeError("q: float32, float16 or bfloat16 is expected, got %s" % q.dtype)
+    _tensor("q", q, q.dtype, (None, None, None), inner=2)
+    T, Hk, dk = q.shape
+    _tensor("k", k, q.dtype, (T, Hk, dk), q.device, inner=2)
+    _tensor("v", v, q.dtype, (T, None, None), q.device, inner=2)
+    Hv, dv = v.shape[1:]
+    _tensor("g", g, torch.float32, (T, Hv), q.device, inner=1)
+    _tensor("beta", beta, torch.float32, (T, Hv), q.device, inner=1)
+    _tensor("o", o, q.dtype, (T, Hv, dv), q.device, inner=2)
+    if state is not None:
+        _tensor("state", state, torch.float32, (None, Hv, dk, dv), q.device)
+    ld = [t.stride(0) if T > 1 else t[0].numel() if T else t.shape[1] * (t.shape[2] if t.dim() == 3 else 1) for t in (q, k, v, g, beta, o)]
+    return csb_delta_shape_t(T, 0 if state is None else state.shape[0], sequences, Hk, Hv, dk, dv, types[q.dtype], *ld, scale or 0.0)
+
+
+def csb_gated_delta_forward(q, k, v, g, beta, o, state=None, seq_begin=None, slot=None, fresh=None, scale=None, flags: int = 0, workspace=None,
+                            stream=None) -> None:
+    """The gated delta rule over sequences packed behind one another (see csb.h); o and, where given, state are written.
+
+    q, k [tokens, k_heads, k_dim], v, o [tokens, v_heads, v_dim] (float32, float16 or bfloat16); g, beta float32 [tokens,
+    v_heads]; state float32 [slots, v_heads, k_dim, v_dim]; seq_begin int32 [sequences + 1] (None: one sequence of all
+    tokens); slot int32 [sequences]; fresh uint8 [sequences].  scale None stands for 1 / sqrt(k_dim)."""
+    import torch
+    n = 1 if seq_begin is None else _tensor("seq_begin", seq_begin, torch.int32, (None,)).shape[0] - 1
+    if n < 0:
+        raise ValueError("seq_begin: sequences + 1 entries are expected, got none")
+    shape = _delta_shape(q, k, v, g, beta, o, state, n, scale)
+    if slot is not None:
+        _tensor("slot", slot, torch.int32, (n,), q.device)
+    if fresh is not None:
+        _tensor("fresh", fresh, torch.uint8, (n,), q.device)
+    buf, size = _scratch(int(lib.csb_gated_delta_workspace_bytes(C.byref(shape))), workspace, q.device, stream)
+    _check(lib.csb_gated_delta_forward(C.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(o), _ptr(state), _ptr(seq_begin), _ptr(slot),
+                                       _ptr(fresh), _ptr(buf), size, flags, _stream(stream)))
+
+
+def csb_gated_delta_step(q, k, v, g, beta, o, state, slot=None, scale=None, flags: int = 0, stream=None) -> None:
+    """The gated delta rule for one token of each of q.shape[0] sequences: tensors as for csb_gated_delta_forward, the
+    states in slots of `state` (slot int32 [tokens], None: slot i for token i; a negative one leaves its token out)."""
+    import torch
+    shape = _delta_shape(q, k, v, g, beta, o, state, q.shape[0], scale)
+    if slot is not None:
+        _tensor("slot", slot, torch.int32, (q.shape[0],), q.device)
+    _check(lib.csb_gated_delta_step(C.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(o), _ptr(state), _ptr(slot), flags, _stream(stream)))
 
 
 # shorter aliases

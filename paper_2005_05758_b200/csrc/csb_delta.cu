@@ -1,0 +1,271 @@
+// The gated delta rule, token by token: per value head a state S [k_dim x v_dim] in fp32,
+//   S <- e^g S;  S <- S + k (beta (v - S^T k))^T;  o = scale S^T q.
+// A CTA holds a slab of columns of one head's state in registers from the first token of a sequence to the last: the
+// columns of S do not meet.  Both products with the old state are taken in one pass over it, since
+//   o = scale (e^g S_old^T q + (k . q) w) with w = beta (v - e^g S_old^T k),
+// so a token costs one sum over the rows (within a warp by shuffles, across warps through shared memory).
+// For one token a sequence the kernel is bound by reading and writing the states once.
+#include <algorithm>
+#include <cmath>
+
+#include "csb_host.hpp"
+#include "csb_delta.hpp"
+#include "csb_device.cuh"
+#include "csb_values.cuh"
+
+namespace csb {
+
+constexpr int kDeltaMaxDim = 256;       // of keys
+constexpr int kDeltaMaxWarps = 16;
+
+// The slot of sequence i, or -1 where the call leaves it alone: a negative or too large slot, or one that an earlier
+// sequence of the call has.  All threads of the block take part.
+__device__ long long delta_slot(const DeltaArgs& a, int i) {
+    if (!a.slot) return i < a.slots ? i : -1;
+    const int mine = a.slot[i];
+    int taken = 0;
+    for (int j = threadIdx.x; j < i; j += blockDim.x) taken |= a.slot[j] == mine;
+    if (__syncthreads_or(taken) || mine < 0 || mine >= a.slots) return -1;
+    return mine;
+}
+
+// Lanes are cut into groups of LC that hold a row of the slab together, four columns each: with VEC behind each other
+// (16-byte loads), else LC apart.  Rows go round the groups of all warps, NR of them to each.
+template <typename T, int NR, bool VEC>
+__global__ void __launch_bounds__(kDeltaMaxWarps * 32) csb_delta_recurrent_kernel(const DeltaArgs a, int LC, int slabs) {
+    __shared__ float kq[2][2][kDeltaMaxDim];
+    __shared__ __align__(16) float red[2][kDeltaMaxWarps][2][128];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int seq = (int)(blockIdx.x / slabs), slab = (int)(blockIdx.x % slabs), h = blockIdx.y, hk = h / (a.v_heads / a.k_heads);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lc = lane & (LC - 1), per = 32 / LC;
+    const int row0 = warp * per + lane / LC, row_step = warps * per;
+    const int c0 = slab * LC * 4;
+    long long t0 = a.step ? seq : 0, t1 = a.step ? seq + 1 : a.tokens;
+    if (a.seq_begin) {
+        t0 = min(max((long long)a.seq_begin[seq], 0ll), a.tokens);
+        t1 = min(max((long long)a.seq_begin[seq + 1], t0), a.tokens);
+    }
+    int col[4];
+    bool there[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        col[j] = c0 + (VEC ? 4 * lc + j : lc + j * LC);
+        there[j] = col[j] < a.v_dim;
+    }
+    long long slot = -1;
+    if (a.state) {
+        slot = delta_slot(a, seq);
+        if (slot < 0) return;
+    }
+    if (t0 >= t1) return;
+    float S[NR][4];
+    float* home = a.state + ((slot < 0 ? 0 : slot) * a.v_heads + h) * (long long)a.k_dim * a.v_dim;
+    const bool from_zero = slot < 0 || (a.fresh && a.fresh[seq]);
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+        const int r = row0 + i * row_step;
+        const bool mine = r < a.k_dim && !from_zero;
+        const float* p = home + (long long)r * a.v_dim;
+        if (VEC) {
+            const float4 f = mine && there[0] ? *reinterpret_cast<const float4*>(p + col[0]) : make_float4(0.f, 0.f, 0.f, 0.f);
+            S[i][0] = f.x; S[i][1] = f.y; S[i][2] = f.z; S[i][3] = f.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) S[i][j] = mine && there[j] ? p[col[j]] : 0.f;
+        }
+    }
+    const T *qp = static_cast<const T*>(a.q) + hk * a.k_dim, *kp = static_cast<const T*>(a.k) + hk * a.k_dim;
+    const T* vp = static_cast<const T*>(a.v) + h * a.v_dim;
+    T* op = static_cast<T*>(a.o) + h * a.v_dim;
+    for (long long t = t0; t < t1; ++t) {
+        const int at = (int)((t - t0) & 1);
+        for (int i = threadIdx.x; i < a.k_dim; i += blockDim.x) {
+            kq[at][0][i] = to_float(kp[t * a.ldk + i]);
+            kq[at][1][i] = to_float(qp[t * a.ldq + i]);
+        }
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = there[j] ? to_float(vp[t * a.ldv + col[j]]) : 0.f;
+        const float decay = expf(a.g[t * a.ldg + h]), beta = a.beta[t * a.ldb + h];
+        __syncthreads();
+        float kk = 0.f, qq = 0.f, dot = 0.f;
+        for (int i = lane; i < a.k_dim; i += 32) {
+            const float x = kq[at][0][i], y = kq[at][1][i];
+            kk += x * x; qq += y * y; dot += x * y;
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            kk += __shfl_xor_sync(0xffffffffu, kk, d); qq += __shfl_xor_sync(0xffffffffu, qq, d); dot += __shfl_xor_sync(0xffffffffu, dot, d);
+        }
+        const float kn = a.normalize ? 1.f / sqrtf(kk + kDeltaEps) : 1.f, qn = a.scale * (a.normalize ? 1.f / sqrtf(qq + kDeltaEps) : 1.f);
+        float u[4] = {0.f, 0.f, 0.f, 0.f}, w[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int r = row0 + i * row_step;
+            if (r >= a.k_dim) break;
+            const float x = kq[at][0][r], y = kq[at][1][r];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { u[j] = fmaf(x, S[i][j], u[j]); w[j] = fmaf(y, S[i][j], w[j]); }
+        }
+        for (int d = LC; d < 32; d <<= 1)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { u[j] += __shfl_xor_sync(0xffffffffu, u[j], d); w[j] += __shfl_xor_sync(0xffffffffu, w[j], d); }
+        if (lane < LC) {
+            *reinterpret_cast<float4*>(&red[at][warp][0][4 * lc]) = make_float4(u[0], u[1], u[2], u[3]);
+            *reinterpret_cast<float4*>(&red[at][warp][1][4 * lc]) = make_float4(w[0], w[1], w[2], w[3]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[j] = w[j] = 0.f;
+        for (int i = 0; i < warps; ++i) {
+            const float4 x = *reinterpret_cast<const float4*>(&red[at][i][0][4 * lc]), y = *reinterpret_cast<const float4*>(&red[at][i][1][4 * lc]);
+            u[0] += x.x; u[1] += x.y; u[2] += x.z; u[3] += x.w;
+            w[0] += y.x; w[1] += y.y; w[2] += y.z; w[3] += y.w;
+        }
+        float out[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float add = beta * (v[j] - decay * kn * u[j]);          // the row that goes in along the normalised key
+            out[j] = qn * (decay * w[j] + kn * dot * add);
+            u[j] = kn * add;
+        }
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int r = row0 + i * row_step;
+            if (r >= a.k_dim) break;
+            const float x = kq[at][0][r];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) S[i][j] = fmaf(x, u[j], decay * S[i][j]);
+        }
+        if (warp == 0 && lane < LC) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (there[j]) op[t * a.ldo + col[j]] = from_float<T>(out[j]);
+        }
+    }
+    if (slot < 0) return;
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+        const int r = row0 + i * row_step;
+        if (r >= a.k_dim) break;
+        float* p = home + (long long)r * a.v_dim;
+        if (VEC) {
+            if (there[0]) *reinterpret_cast<float4*>(p + col[0]) = make_float4(S[i][0], S[i][1], S[i][2], S[i][3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (there[j]) p[col[j]] = S[i][j];
+        }
+    }
+}
+
+#define CSB_CUDA(call)                                                                     \
+    do {                                                                                   \
+        cudaError_t e_ = (call);                                                           \
+        if (e_ != cudaSuccess) {                                                           \
+            set_error("%s failed: %s", #call, cudaGetErrorString(e_));                     \
+            return e_ == cudaErrorMemoryAllocation ? CSB_ERR_ALLOC : CSB_ERR_CUDA;         \
+        }                                                                                  \
+    } while (0)
+
+template <typename T>
+static int launch_recurrent(const DeltaArgs& a, void* stream) {
+    // a slab is as wide as the head, up to 128 columns; narrower where that leaves SMs without work
+    int LC = 1;
+    while (LC < 32 && LC * 4 < a.v_dim) LC *= 2;
+    while (LC > 8 && (int64_t)a.sequences * a.v_heads * ((a.v_dim + LC * 4 - 1) / (LC * 4)) < 148) LC /= 2;
+    const int slabs = (a.v_dim + LC * 4 - 1) / (LC * 4), per = 32 / LC;
+    int NR = 4;
+    while (NR < 16 && (a.k_dim + per * NR - 1) / (per * NR) > 8) NR *= 2;
+    const int warps = (a.k_dim + per * NR - 1) / (per * NR);
+    const bool vec = a.v_dim % 4 == 0 && reinterpret_cast<uintptr_t>(a.state) % 16 == 0;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(a.sequences * (int64_t)slabs), (unsigned)a.v_heads); cfg.blockDim = dim3((unsigned)warps * 32); cfg.stream = (cudaStream_t)stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    void (*kernel)(const DeltaArgs, int, int) =
+        vec ? (NR == 4 ? csb_delta_recurrent_kernel<T, 4, true> : NR == 8 ? csb_delta_recurrent_kernel<T, 8, true> : csb_delta_recurrent_kernel<T, 16, true>)
+            : (NR == 4 ? csb_delta_recurrent_kernel<T, 4, false> : NR == 8 ? csb_delta_recurrent_kernel<T, 8, false> : csb_delta_recurrent_kernel<T, 16, false>);
+    CSB_CUDA(cudaLaunchKernelEx(&cfg, kernel, a, LC, slabs));
+    return CSB_OK;
+}
+
+// Checks what both entry points are given; CSB_OK with out->sequences = 0 where there is nothing to do.
+static int delta_args(const csb_delta_shape_t* s, const void* q, const void* k, const void* v, const float* g, const float* beta, void* o, float* state,
+                      unsigned flags, DeltaArgs* out) {
+    if (!s) { set_error("shape is NULL"); return CSB_ERR_INVALID_ARG; }
+    if (s->tokens < 0 || s->sequences < 0 || s->slots < 0 || s->k_heads < 1 || s->v_heads < 1 || s->k_dim < 1 || s->v_dim < 1) {
+        set_error("tokens=%lld sequences=%d slots=%lld k_heads=%d v_heads=%d k_dim=%d v_dim=%d", (long long)s->tokens, s->sequences, (long long)s->slots,
+                  s->k_heads, s->v_heads, s->k_dim, s->v_dim);
+        return CSB_ERR_INVALID_ARG;
+    }
+    if (s->dtype != CSB_F32 && s->dtype != CSB_F16 && s->dtype != CSB_BF16) { set_error("dtype %d", s->dtype); return CSB_ERR_DTYPE; }
+    if (flags & ~(unsigned)CSB_FLAG_NORMALIZE) { set_error("flags %u: CSB_FLAG_NORMALIZE alone is known here", flags); return CSB_ERR_INVALID_ARG; }
+    if (s->v_heads % s->k_heads) { set_error("%d value heads do not share %d key heads evenly", s->v_heads, s->k_heads); return CSB_ERR_SHAPE; }
+    const int64_t wk = (int64_t)s->k_heads * s->k_dim, wv = (int64_t)s->v_heads * s->v_dim;
+    if (s->ldq < wk || s->ldk < wk || s->ldv < wv || s->ldo < wv || s->ldg < s->v_heads || s->ldb < s->v_heads) {
+        set_error("a row stride is shorter than its row: q %lld k %lld (rows of %lld), v %lld o %lld (%lld), g %lld beta %lld (%d)", (long long)s->ldq,
+                  (long long)s->ldk, (long long)wk, (long long)s->ldv, (long long)s->ldo, (long long)wv, (long long)s->ldg, (long long)s->ldb, s->v_heads);
+        return CSB_ERR_SHAPE;
+    }
+    if (!(s->scale >= 0.f) || std::isinf(s->scale)) { set_error("scale %g", (double)s->scale); return CSB_ERR_INVALID_ARG; }
+    if (s->k_dim > kDeltaMaxDim || s->v_heads > 65535 || s->v_dim > 65536 || s->tokens > 0x7fffffff) {
+        set_error("k_dim up to %d, v_dim up to 65536, heads up to 65535 and tokens up to 2^31 - 1 are supported", kDeltaMaxDim);
+        return CSB_ERR_UNSUPPORTED;
+    }
+    if ((int64_t)s->sequences * ((s->v_dim + 3) / 4) > 0x7fffffff) { set_error("%d sequences with values of %d are more than a grid has", s->sequences, s->v_dim); return CSB_ERR_UNSUPPORTED; }
+    DeltaArgs a{};
+    if (s->tokens == 0 || s->sequences == 0) { *out = a; return CSB_OK; }
+    if (!q || !k || !v || !g || !beta || !o) { set_error("q, k, v, g, beta or o is NULL"); return CSB_ERR_INVALID_ARG; }
+    a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.o = o; a.state = state;
+    a.tokens = s->tokens; a.slots = s->slots; a.ldq = s->ldq; a.ldk = s->ldk; a.ldv = s->ldv; a.ldg = s->ldg; a.ldb = s->ldb; a.ldo = s->ldo;
+    a.sequences = s->sequences; a.k_heads = s->k_heads; a.v_heads = s->v_heads; a.k_dim = s->k_dim; a.v_dim = s->v_dim;
+    a.scale = s->scale > 0.f ? s->scale : (float)(1.0 / std::sqrt((double)s->k_dim));
+    a.normalize = (flags & CSB_FLAG_NORMALIZE) != 0;
+    *out = a;
+    return CSB_OK;
+}
+
+static int recurrent_any(int dtype, const DeltaArgs& a, void* stream) {
+    return dtype == CSB_F32 ? launch_recurrent<float>(a, stream) : dtype == CSB_F16 ? launch_recurrent<__half>(a, stream) : launch_recurrent<__nv_bfloat16>(a, stream);
+}
+
+}  // namespace csb
+
+using namespace csb;
+
+extern "C" {
+
+int64_t csb_gated_delta_workspace_bytes(const csb_delta_shape_t* shape) {
+    return shape ? 16 : 0;
+}
+
+int csb_gated_delta_forward(const csb_delta_shape_t* shape, const void* q, const void* k, const void* v, const float* g, const float* beta, void* o,
+                            float* state, const int32_t* seq_begin, const int32_t* slot, const uint8_t* fresh, void* workspace, int64_t workspace_bytes,
+                            unsigned flags, void* stream) {
+    clear_error();
+    DeltaArgs a;
+    const int rc = delta_args(shape, q, k, v, g, beta, o, state, flags, &a);
+    if (rc != CSB_OK || a.sequences == 0) return rc;
+    if (!seq_begin && shape->sequences != 1) { set_error("seq_begin is NULL with %d sequences", shape->sequences); return CSB_ERR_INVALID_ARG; }
+    const int64_t need = csb_gated_delta_workspace_bytes(shape);
+    if (need && (!workspace || workspace_bytes < need)) { set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need); return CSB_ERR_INVALID_ARG; }
+    a.seq_begin = seq_begin; a.slot = slot; a.fresh = fresh;
+    return recurrent_any(shape->dtype, a, stream);
+}
+
+int csb_gated_delta_step(const csb_delta_shape_t* shape, const void* q, const void* k, const void* v, const float* g, const float* beta, void* o,
+                         float* state, const int32_t* slot, unsigned flags, void* stream) {
+    clear_error();
+    DeltaArgs a;
+    const int rc = delta_args(shape, q, k, v, g, beta, o, state, flags, &a);
+    if (rc != CSB_OK || a.sequences == 0) return rc;
+    if (!state) { set_error("state is NULL"); return CSB_ERR_INVALID_ARG; }
+    if (shape->tokens != shape->sequences) { set_error("%lld tokens of %d sequences: a step takes one of each", (long long)shape->tokens, shape->sequences); return CSB_ERR_SHAPE; }
+    a.slot = slot; a.step = 1;
+    return recurrent_any(shape->dtype, a, stream);
+}
+
+}  // extern "C"

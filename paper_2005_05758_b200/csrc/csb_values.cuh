@@ -1,0 +1,70 @@
+// Values of the three storage types that users' tensors come in, and the tensor-core steps and splits that the kernels on
+// them share.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+namespace csb {
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// N values behind each other, one load of up to 16 bytes at a time; the address is a multiple of the load's size.
+template <int N>
+__device__ __forceinline__ void load_values(const float* p, float (&v)[N]) {
+    static_assert(N % 4 == 0, "whole loads");
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const float4 f = *reinterpret_cast<const float4*>(p + i);
+        v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
+    }
+}
+__device__ __forceinline__ float2 pair_to_float(uint32_t w, __half) {
+    __half2 h; *reinterpret_cast<uint32_t*>(&h) = w;
+    return __half22float2(h);
+}
+__device__ __forceinline__ float2 pair_to_float(uint32_t w, __nv_bfloat16) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <int N, typename T>
+__device__ __forceinline__ void load_values(const T* p, float (&v)[N]) {
+    static_assert(N == 4 || N % 8 == 0, "whole loads");
+    if constexpr (N == 4) {
+        const uint2 w = *reinterpret_cast<const uint2*>(p);
+        const float2 a = pair_to_float(w.x, T()), b = pair_to_float(w.y, T());
+        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 8) {
+            const uint4 w = *reinterpret_cast<const uint4*>(p + i);
+            const float2 a = pair_to_float(w.x, T()), b = pair_to_float(w.y, T()), c = pair_to_float(w.z, T()), d = pair_to_float(w.w, T());
+            v[i] = a.x; v[i + 1] = a.y; v[i + 2] = b.x; v[i + 3] = b.y; v[i + 4] = c.x; v[i + 5] = c.y; v[i + 6] = d.x; v[i + 7] = d.y;
+        }
+    }
+}
+
+// x = hi + lo with hi and lo of 11 bits each (tf32): 22 bits of x stay.
+__device__ __forceinline__ uint32_t tf32_of(float x) {
+    uint32_t r;
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ void split_tf32(float x, uint32_t& hi, uint32_t& lo) {
+    hi = tf32_of(x);
+    lo = tf32_of(x - __uint_as_float(hi));
+}
+// D[16 x 8] += A[16 x 8] B[8 x 8].  Lane 4g + t holds A at (g, t), (g + 8, t), (g, t + 4), (g + 8, t + 4), B at (t, g),
+// (t + 4, g) and D at (g, 2t), (g, 2t + 1), (g + 8, 2t), (g + 8, 2t + 1).
+__device__ __forceinline__ void mma_tf32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+}  // namespace csb
