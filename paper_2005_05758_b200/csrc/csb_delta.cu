@@ -10,6 +10,7 @@
 
 #include "csb_host.hpp"
 #include "csb_delta.hpp"
+#include "csb_delta_slot.cuh"
 #include "csb_device.cuh"
 #include "csb_values.cuh"
 
@@ -17,17 +18,6 @@ namespace csb {
 
 constexpr int kDeltaMaxDim = 256;       // of keys
 constexpr int kDeltaMaxWarps = 16;
-
-// The slot of sequence i, or -1 where the call leaves it alone: a negative or too large slot, or one that an earlier
-// sequence of the call has.  All threads of the block take part.
-__device__ long long delta_slot(const DeltaArgs& a, int i) {
-    if (!a.slot) return i < a.slots ? i : -1;
-    const int mine = a.slot[i];
-    int taken = 0;
-    for (int j = threadIdx.x; j < i; j += blockDim.x) taken |= a.slot[j] == mine;
-    if (__syncthreads_or(taken) || mine < 0 || mine >= a.slots) return -1;
-    return mine;
-}
 
 // Lanes are cut into groups of LC that hold a row of the slab together, four columns each: with VEC behind each other
 // (16-byte loads), else LC apart.  Rows go round the groups of all warps, NR of them to each.
@@ -232,14 +222,18 @@ static int recurrent_any(int dtype, const DeltaArgs& a, void* stream) {
     return dtype == CSB_F32 ? launch_recurrent<float>(a, stream) : dtype == CSB_F16 ? launch_recurrent<__half>(a, stream) : launch_recurrent<__nv_bfloat16>(a, stream);
 }
 
+// Sequences of few tokens each go token by token: a chunk costs as much as its tokens when it has about eight of them.
+static bool short_sequences(const csb_delta_shape_t* s) { return s->tokens <= 8 * (int64_t)s->sequences; }
+
 }  // namespace csb
 
 using namespace csb;
 
 extern "C" {
 
-int64_t csb_gated_delta_workspace_bytes(const csb_delta_shape_t* shape) {
-    return shape ? 16 : 0;
+int64_t csb_gated_delta_workspace_bytes(const csb_delta_shape_t* s) {
+    if (!s || s->tokens <= 0 || s->sequences <= 0 || s->k_heads < 1 || s->v_heads < 1 || s->k_dim < 1 || s->k_dim > kDeltaMaxDim || short_sequences(s)) return 0;
+    return delta_chunk_bytes(s->tokens, s->sequences, s->k_heads, s->v_heads, s->k_dim, s->dtype);
 }
 
 int csb_gated_delta_forward(const csb_delta_shape_t* shape, const void* q, const void* k, const void* v, const float* g, const float* beta, void* o,
@@ -253,7 +247,7 @@ int csb_gated_delta_forward(const csb_delta_shape_t* shape, const void* q, const
     const int64_t need = csb_gated_delta_workspace_bytes(shape);
     if (need && (!workspace || workspace_bytes < need)) { set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need); return CSB_ERR_INVALID_ARG; }
     a.seq_begin = seq_begin; a.slot = slot; a.fresh = fresh;
-    return recurrent_any(shape->dtype, a, stream);
+    return need ? launch_delta_chunks(shape->dtype, a, workspace, stream) : recurrent_any(shape->dtype, a, stream);
 }
 
 int csb_gated_delta_step(const csb_delta_shape_t* shape, const void* q, const void* k, const void* v, const float* g, const float* beta, void* o,

@@ -3,6 +3,8 @@
 
 #include <stdint.h>
 
+#include "csb_internal.hpp"
+
 namespace csb {
 
 struct DeltaArgs {
@@ -19,5 +21,18 @@ struct DeltaArgs {
 };
 
 constexpr float kDeltaEps = 1e-6f;      // added to the sum of squares that a query or key is divided by the root of
+
+// Chunks of tokens (csb_delta_chunk.cu).  Chunk c of sequence i has record begin_i / kChunk + i + c, which leaves room for the
+// last chunk of every sequence without knowing any length on the host.
+constexpr int kChunk = 32;
+struct DeltaChunkArgs {
+    uint8_t *keys, *heads;              // [records][k_heads] operands of a chunk, [records][v_heads] its matrices and factors
+    long long records;
+    int key_bytes, tiles_a_cta, groups; // of a key record; tiles of 16 value columns of a CTA, CTAs of a head
+};
+
+// csb_delta_chunk.cu
+int64_t delta_chunk_bytes(int64_t tokens, int64_t sequences, int k_heads, int v_heads, int k_dim, int dtype);
+int launch_delta_chunks(int dtype, const DeltaArgs& a, void* workspace, void* stream);
 
 }  // namespace csb

@@ -1,0 +1,620 @@
+// The gated delta rule in chunks of 32 tokens, on tensor cores.  With G_t the sum of the log-decays from the chunk's first
+// token to t, S the state in front of the chunk and all sums over the chunk's tokens:
+//   V'_t = sum_s Tinv[t][s] beta_s (v_s - e^(G_s) S^T k_s),   Tinv the inverse of 1 + [s < t] beta_t e^(G_t - G_s) k_t . k_s
+//   o_t  = scale (e^(G_t) S^T q_t + sum_{s <= t} e^(G_t - G_s) (q_t . k_s) V'_s)
+//   S   <- e^(G_end) S + sum_s e^(G_end - G_s) k_s V'_s^T.
+// What does not need S is done for all chunks at once by csb_delta_prepare_kernel, which leaves a record a chunk: the keys and
+// queries as binary16 (their rows scaled by powers of two; fp32 ones as two halves), the 32 x 32 matrices and a few
+// factors a token.  csb_delta_chunk_kernel goes through the chunks of a sequence.  A warp owns 16 columns of a head's
+// state, as S^T in the accumulators of mma.sync tiles: these are, as they stand, the operands of the next product, so the
+// whole chain state -> V' -> output and next state stays in the registers of one warp, and no warp waits for
+// another's values.  (On tcgen05 every link of the chain would go through TMEM and shared memory; the chain's
+// latency, not the tensor rate, bounds a sequence.)
+//
+// Precision: the fp32 operand of a product (S, V') is split into two binary16 halves after its row is scaled by a power of two,
+// so 22 bits of it stay, whatever its size; 16-bit keys and queries are exact in one half.  Increments of the state are
+// summed apart and added in fp32.
+//
+// Chunks that these forms do not hold go token by token in fp32 (walk_chunk_tokens): log-decays above 0, whose factors are not
+// bounded, and values that are not finite, which products with zeros would carry to tokens in front of them.
+#include <algorithm>
+#include <cmath>
+
+#include "csb_host.hpp"
+#include "csb_delta_slot.cuh"
+#include "csb_device.cuh"
+#include "csb_values.cuh"
+
+namespace csb {
+
+// A head's record: binary16 [kChunk][kChunk] four times, rows of 64 bytes whose 16-byte units are exchanged by matrix_at,
+// then factors.
+enum : int { kSolveHi = 0, kSolveLo = 2048, kInnerHi = 4096, kInnerLo = 6144, kFactors = 8192 };
+struct DeltaFactors {
+    float put[kChunk];                  // the scale of the solve matrix's column: V enters as put V - keep S^T k
+    float keep[kChunk];
+    float from_state[kChunk];           // of S^T q in o
+    float from_chunk[kChunk];           // of the chunk's own part in o
+    float to_end[kChunk];               // e^(G_end - G_t)
+    float whole;                        // e^(G_end)
+    int irregular;
+    int pad[2];
+};
+constexpr int kHeadBytes = (kFactors + (int)sizeof(DeltaFactors) + 511) / 512 * 512;
+constexpr float kLargest = 3.402823466e38f;
+
+__device__ __forceinline__ int matrix_at(int row, int col) { return row * 64 + (((col >> 3) ^ (row >> 1 & 3)) << 4) + (col & 7) * 2; }
+template <int DKP>
+__device__ __forceinline__ int operand_at(int row, int col) { return row * DKP * 2 + (((col >> 3) ^ (row & 7)) << 4) + (col & 7) * 2; }
+
+// 2^n that takes a largest magnitude into [2^TOP, 2^(TOP + 1)), and its inverse.
+template <int TOP>
+__device__ __forceinline__ float scale_of(float largest, float& inverse) {
+    const int e = (int)(__float_as_uint(largest) >> 23), s = min(254 + TOP - e, 253);
+    inverse = __uint_as_float((uint32_t)(254 - s) << 23);
+    return __uint_as_float((uint32_t)s << 23);
+}
+
+__device__ __forceinline__ void sequence_range(const DeltaArgs& a, int i, long long& t0, long long& t1) {
+    t0 = 0; t1 = a.tokens;
+    if (a.seq_begin) {
+        t0 = min(max((long long)a.seq_begin[i], 0ll), a.tokens);
+        t1 = min(max((long long)a.seq_begin[i + 1], t0), a.tokens);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------
+
+constexpr int kPrepareWarps = 4;
+template <int DKP, bool LO>
+struct PrepareSmem {
+    uint8_t rows[LO ? 2 : 1][2][kChunk * DKP * 2];      // hi (and lo): keys, queries
+    float dots[2 * kChunk][kChunk + 1];                 // of scaled rows: key . key, query . key
+    float norm[2 * kChunk];                             // what a scaled row is to be multiplied by
+    float lower[kPrepareWarps][kChunk][kChunk + 4];
+    double sum[kPrepareWarps][kChunk];
+    int odd;
+};
+
+template <typename T, int DKP>
+__global__ void __launch_bounds__(kPrepareWarps * 32) csb_delta_prepare_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
+    constexpr bool LO = sizeof(T) == 4;
+    extern __shared__ __align__(512) uint8_t raw[];
+    PrepareSmem<DKP, LO>& M = *reinterpret_cast<PrepareSmem<DKP, LO>*>(raw);
+    pdl_launch_dependents();
+    pdl_wait();
+    const long long rec = blockIdx.x;
+    const int hk = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int lo = 0;
+    long long t0, t1;
+    for (int hi = a.sequences; hi - lo > 1;) {           // the last sequence whose first record is not behind this one
+        const int mid = lo + (hi - lo) / 2;
+        sequence_range(a, mid, t0, t1);
+        if (t0 / kChunk + mid <= rec) lo = mid; else hi = mid;
+    }
+    sequence_range(a, lo, t0, t1);
+    const long long c = rec - (t0 / kChunk + lo), first = t0 + c * kChunk;
+    if (c < 0 || first >= t1) return;
+    const int n = (int)min((long long)kChunk, t1 - first);
+    if (threadIdx.x == 0) M.odd = 0;
+    __syncthreads();
+
+    // rows 0 .. 31 are keys, 32 .. 63 queries; a warp takes 16 of them, a lane pairs of values 64 apart
+    constexpr int P = DKP / 64;
+    const T *kp = static_cast<const T*>(a.k) + (long long)hk * a.k_dim, *qp = static_cast<const T*>(a.q) + (long long)hk * a.k_dim;
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+        const int row = warp * 16 + i, t = row & (kChunk - 1);
+        const T* p = row < kChunk ? kp + (first + t) * a.ldk : qp + (first + t) * a.ldq;
+        float x[P][2], largest = 0.f, squares = 0.f;
+        bool finite = true;
+#pragma unroll
+        for (int j = 0; j < P; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int col = 64 * j + 2 * lane + e;
+                const float v = t < n && col < a.k_dim ? to_float(p[col]) : 0.f;
+                x[j][e] = v;
+                largest = fmaxf(largest, fabsf(v));
+                finite &= fabsf(v) <= kLargest;
+                squares = fmaf(v, v, squares);
+            }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, d));
+            squares += __shfl_xor_sync(0xffffffffu, squares, d);
+        }
+        float back;
+        const float by = scale_of<0>(largest, back);
+        if (lane == 0) M.norm[row] = a.normalize ? back / sqrtf(squares + kDeltaEps) : back;
+        if (!finite || squares > kLargest) M.odd = 1;
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const int at = operand_at<DKP>(t, 64 * j + 2 * lane), which = row >= kChunk;
+            uint32_t h, l;
+            split_pair(x[j][0] * by, x[j][1] * by, h, l);
+            *reinterpret_cast<uint32_t*>(&M.rows[0][which][at]) = h;
+            if (LO) *reinterpret_cast<uint32_t*>(&M.rows[LO ? 1 : 0][which][at]) = l;
+        }
+    }
+    __syncthreads();
+    {
+        uint4* out = reinterpret_cast<uint4*>(w.keys + (rec * a.k_heads + hk) * w.key_bytes);
+        const uint4* in = reinterpret_cast<const uint4*>(&M.rows[0][0][0]);
+        for (int i = threadIdx.x; i < (LO ? 4 : 2) * kChunk * DKP * 2 / 16; i += kPrepareWarps * 32) out[i] = in[i];
+    }
+    {
+        // rows 16 warp .. + 15 of [keys; queries] times the keys
+        float d[4][4] = {};
+        const int which = warp >> 1, row = (warp & 1) * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
+        const uint32_t base_a = smem_u32(&M.rows[0][which][0]), base_b = smem_u32(&M.rows[0][0][0]);
+        const uint32_t at_a = row * DKP * 2 + (((lane >> 4) ^ (row & 7)) << 4);
+        const int tok = (lane >> 4) * 8 + (lane & 7);
+        const uint32_t at_b = tok * DKP * 2 + (((lane >> 3 & 1) ^ (tok & 7)) << 4);
+        constexpr uint32_t kLoAt = 2 * kChunk * DKP * 2;
+#pragma unroll
+        for (int j = 0; j < DKP / 16; ++j) {
+            uint32_t ah[4], b[2][4];
+            load_matrices(ah, base_a + (at_a ^ (32 * j)));
+            load_matrices(b[0], base_b + (at_b ^ (32 * j)));
+            load_matrices(b[1], (base_b + (at_b ^ (32 * j))) + 16 * DKP * 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(d[i], ah, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+            if (LO) {
+                uint32_t al[4];
+                load_matrices(al, (base_a + (at_a ^ (32 * j))) + kLoAt);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mma_f16(d[i], al, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+                load_matrices(b[0], (base_b + (at_b ^ (32 * j))) + kLoAt);
+                load_matrices(b[1], (base_b + (at_b ^ (32 * j))) + kLoAt + 16 * DKP * 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mma_f16(d[i], ah, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) M.dots[warp * 16 + (lane >> 2) + (k >> 1) * 8][8 * i + 2 * (lane & 3) + (k & 1)] = d[i][k];
+    }
+    __syncthreads();
+
+    // a warp a value head: lane s has column s of the matrices
+    const int each = a.v_heads / a.k_heads;
+    for (int e = warp; e < each; e += kPrepareWarps) {
+        const int h = hk * each + e;
+        uint8_t* out = w.heads + (rec * a.v_heads + h) * kHeadBytes;
+        const bool there = lane < n;
+        const float g = there ? a.g[(first + lane) * a.ldg + h] : 0.f, beta = there ? a.beta[(first + lane) * a.ldb + h] : 0.f;
+        bool odd = M.odd || !(g <= 0.f) || !(fabsf(beta) <= kLargest);
+        // log-decays are summed in 64 bits, where the difference of two large sums is still a small one's; e^-10000 is 0 as e^-inf is
+        double G = g < -10000.f ? -10000.0 : (double)g;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const double before = __shfl_up_sync(0xffffffffu, G, d);
+            if (lane >= d) G += before;
+        }
+        M.sum[warp][lane] = G;
+        float(&A)[kChunk][kChunk + 4] = M.lower[warp];
+        const float norm = M.norm[lane];
+        __syncwarp();
+#pragma unroll 4
+        for (int i = 0; i < kChunk; ++i) {
+            const float decay = lane <= i ? expf((float)(M.sum[warp][i] - G)) : 0.f;
+            const float beta_i = __shfl_sync(0xffffffffu, beta, i);
+            A[i][lane] = lane < i ? beta_i * M.norm[i] * norm * decay * M.dots[i][lane] : 0.f;
+            const float p = decay * M.dots[kChunk + i][lane];
+            const __half hi = __float2half_rn(p);
+            *reinterpret_cast<__half*>(out + kInnerHi + matrix_at(i, lane)) = hi;
+            *reinterpret_cast<__half*>(out + kInnerLo + matrix_at(i, lane)) = __float2half_rn(p - __half2float(hi));
+        }
+        __syncwarp();
+        // column `lane` of the inverse of 1 + A, from the top down
+        float x[kChunk];
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) {
+            float s0 = lane == i ? 1.f : 0.f, s1 = 0.f;
+#pragma unroll
+            for (int m = 0; m < i; m += 4) {
+                const float4 r = *reinterpret_cast<const float4*>(&A[i][m]);
+                s0 = fmaf(-r.x, x[m], s0);
+                if (m + 1 < i) s1 = fmaf(-r.y, x[m + 1], s1);
+                if (m + 2 < i) s0 = fmaf(-r.z, x[m + 2], s0);
+                if (m + 3 < i) s1 = fmaf(-r.w, x[m + 3], s1);
+            }
+            x[i] = s0 + s1;
+        }
+        float largest = 0.f;
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) {
+            x[i] *= M.norm[i] * beta;
+            odd |= !(fabsf(x[i]) <= kLargest);
+            largest = fmaxf(largest, fabsf(x[i]));
+        }
+        float back;
+        const float by = scale_of<8>(largest, back);
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) {
+            const float v = x[i] * by;
+            const __half hi = __float2half_rn(v);
+            *reinterpret_cast<__half*>(out + kSolveHi + matrix_at(i, lane)) = hi;
+            *reinterpret_cast<__half*>(out + kSolveLo + matrix_at(i, lane)) = __float2half_rn(v - __half2float(hi));
+        }
+        DeltaFactors& F = *reinterpret_cast<DeltaFactors*>(out + kFactors);
+        const double end = M.sum[warp][kChunk - 1];
+        const float from = expf((float)G), qn = a.scale * M.norm[kChunk + lane];
+        F.put[lane] = back;
+        F.keep[lane] = back * from * norm;
+        F.from_state[lane] = from * qn;
+        F.from_chunk[lane] = qn;
+        F.to_end[lane] = expf((float)(end - G));
+        odd = __any_sync(0xffffffffu, odd);
+        if (lane == 0) { F.whole = expf((float)end); F.irregular = odd; }
+        __syncwarp();
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void copy_16(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ float quad_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+    return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+    v += __shfl_xor_sync(0xffffffffu, v, 1);
+    return v + __shfl_xor_sync(0xffffffffu, v, 2);
+}
+
+// [16 columns of the head x 32 tokens] in accumulators, as two halves of operands of the next product; rows scaled by by0, by1.
+__device__ __forceinline__ void split_tile(const float (&x)[4][4], float by0, float by1, uint32_t (&hi)[2][4], uint32_t (&lo)[2][4]) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float by = i & 1 ? by1 : by0;
+            const float* p = &x[2 * s + (i >> 1)][(i & 1) * 2];
+            split_pair(p[0] * by, p[1] * by, hi[s][i], lo[s][i]);
+        }
+}
+__device__ __forceinline__ void rows_max(const float (&x)[4][4], float& m0, float& m1) {
+    m0 = m1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        m0 = fmaxf(m0, fmaxf(fabsf(x[i][0]), fabsf(x[i][1])));
+        m1 = fmaxf(m1, fmaxf(fabsf(x[i][2]), fabsf(x[i][3])));
+    }
+    m0 = quad_max(m0); m1 = quad_max(m1);
+}
+// d += x M^T for a 32 x 32 matrix without an upper part; `at` is this lane's place in it, `lo` where its second half lies.
+// (The product of the two second halves is left out: 2^-22.)
+__device__ __forceinline__ void times_lower(float (&d)[4][4], const uint32_t (&hi)[2][4], const uint32_t (&lo)[2][4], uint32_t at, uint32_t lo_at) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int p = s; p < 2; ++p) {
+            uint32_t b[4];
+            load_matrices(b, (at ^ (32 * s)) + p * 16 * 64);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                mma_f16(d[2 * p + i], hi[s], b[2 * i], b[2 * i + 1]);
+                mma_f16(d[2 * p + i], lo[s], b[2 * i], b[2 * i + 1]);
+            }
+            load_matrices(b, (at ^ (32 * s)) + p * 16 * 64 + lo_at);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) mma_f16(d[2 * p + i], hi[s], b[2 * i], b[2 * i + 1]);
+        }
+}
+
+// Tokens [first, first + n) one by one in fp32 on a warp's part of the state.
+template <typename T, int DKP>
+__device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)[DKP / 8][4], int h, int hk, int col0, long long first, int n) {
+    const int lane = threadIdx.x & 31, t = lane & 3;
+    for (long long at = first; at < first + n; ++at) {
+        const T *kp = static_cast<const T*>(a.k) + (long long)hk * a.k_dim + at * a.ldk, *qp = static_cast<const T*>(a.q) + (long long)hk * a.k_dim + at * a.ldq;
+        float kk = 0.f, qq = 0.f, dot = 0.f, u[2] = {0.f, 0.f}, o[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < DKP / 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int c = 8 * j + 2 * t + e;
+                if (c >= a.k_dim) continue;
+                const float x = to_float(kp[c]), y = to_float(qp[c]);
+                kk = fmaf(x, x, kk); qq = fmaf(y, y, qq); dot = fmaf(x, y, dot);
+                u[0] = fmaf(x, S[j][e], u[0]); u[1] = fmaf(x, S[j][2 + e], u[1]);
+                o[0] = fmaf(y, S[j][e], o[0]); o[1] = fmaf(y, S[j][2 + e], o[1]);
+            }
+        kk = quad_sum(kk); qq = quad_sum(qq); dot = quad_sum(dot);
+        const float kn = a.normalize ? 1.f / sqrtf(kk + kDeltaEps) : 1.f, qn = a.scale * (a.normalize ? 1.f / sqrtf(qq + kDeltaEps) : 1.f);
+        const float decay = expf(a.g[at * a.ldg + h]), beta = a.beta[at * a.ldb + h];
+        float add[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int col = col0 + (lane >> 2) + 8 * r;
+            const float seen = decay * kn * quad_sum(u[r]), old = decay * quad_sum(o[r]);
+            const float v = col < a.v_dim ? to_float(static_cast<const T*>(a.v)[at * a.ldv + (long long)h * a.v_dim + col]) : 0.f;
+            add[r] = kn * (beta * (v - seen));
+            if (t == 0 && col < a.v_dim) static_cast<T*>(a.o)[at * a.ldo + (long long)h * a.v_dim + col] = from_float<T>(qn * (old + dot * add[r]));
+        }
+#pragma unroll
+        for (int j = 0; j < DKP / 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int c = 8 * j + 2 * t + e;
+                if (c >= a.k_dim) continue;
+                const float x = to_float(kp[c]);
+                S[j][e] = fmaf(x, add[0], decay * S[j][e]);
+                S[j][2 + e] = fmaf(x, add[1], decay * S[j][2 + e]);
+            }
+    }
+}
+
+template <typename T, int DKP>
+__host__ __device__ constexpr int stage_bytes() { return (sizeof(T) == 4 ? 4 : 2) * kChunk * DKP * 2 + kHeadBytes; }
+constexpr int kStages = 3;
+
+template <typename T, int DKP>
+__global__ void __launch_bounds__(256) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
+    constexpr bool LO = sizeof(T) == 4;
+    constexpr int kStage = stage_bytes<T, DKP>(), kRows = kChunk * DKP * 2;
+    constexpr int kKeyBytes = (LO ? 4 : 2) * kRows;
+    extern __shared__ __align__(512) uint8_t smem[];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int group = (int)(blockIdx.x % w.groups);
+    const long long rest = blockIdx.x / w.groups;
+    const int h = (int)(rest % a.v_heads), seq = (int)(rest / a.v_heads), hk = h / (a.v_heads / a.k_heads);
+    long long t0, t1, slot = -1;
+    sequence_range(a, seq, t0, t1);
+    if (a.state) {
+        slot = delta_slot(a, seq);
+        if (slot < 0) return;
+    }
+    if (t0 >= t1) return;
+    const int col0 = (group * w.tiles_a_cta + warp) * 16;       // (a warp behind the last column works on zeros)
+    float S[DKP / 8][4];
+    float* home = a.state + ((slot < 0 ? 0 : slot) * a.v_heads + h) * (long long)a.k_dim * a.v_dim;
+    const bool from_zero = slot < 0 || (a.fresh && a.fresh[seq]);
+#pragma unroll
+    for (int j = 0; j < DKP / 8; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 8 * j + 2 * t + (i & 1), col = col0 + g + (i >> 1) * 8;
+            S[j][i] = !from_zero && r < a.k_dim && col < a.v_dim ? home[(long long)r * a.v_dim + col] : 0.f;
+        }
+
+    const int chunks = (int)((t1 - t0 + kChunk - 1) / kChunk);
+    const long long rec0 = t0 / kChunk + seq;
+    auto fetch = [&](int c) {
+        if (c < chunks) {
+            const uint32_t to = smem_u32(smem) + (c % kStages) * kStage;
+            const uint8_t *keys = w.keys + ((rec0 + c) * a.k_heads + hk) * w.key_bytes, *head = w.heads + ((rec0 + c) * a.v_heads + h) * kHeadBytes;
+            for (int i = threadIdx.x * 16; i < kKeyBytes; i += blockDim.x * 16) copy_16(to + i, keys + i);
+            for (int i = threadIdx.x * 16; i < kFactors + (int)sizeof(DeltaFactors); i += blockDim.x * 16) copy_16(to + kKeyBytes + i, head + i);
+        }
+        copies_commit();
+    };
+    // values of this lane's columns g, g + 8 for its tokens 8i + 2t, 8i + 2t + 1
+    float v[4][4];
+    auto values = [&](int c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const long long at = t0 + (long long)c * kChunk + 8 * i + 2 * t + (k & 1);
+                const int col = col0 + g + (k >> 1) * 8;
+                v[i][k] = at < t1 && col < a.v_dim ? to_float(static_cast<const T*>(a.v)[at * a.ldv + (long long)h * a.v_dim + col]) : 0.f;
+            }
+    };
+    fetch(0);
+    fetch(1);
+    values(0);
+    // this lane's places in the operands (see load_matrices): rows are tokens, units 32 bytes a step apart
+    const int tok = (lane >> 4) * 8 + (lane & 7);
+    const uint32_t row_at = tok * DKP * 2 + (((lane >> 3 & 1) ^ (tok & 7)) << 4), row_at_t = lane * DKP * 2 + ((lane & 7) << 4);
+    const uint32_t mat_at = matrix_at(tok, (lane >> 3 & 1) * 8);
+    for (int c = 0; c < chunks; ++c) {
+        copies_wait<1>();
+        __syncthreads();                                        // chunk c is there, and everybody is done with chunk c - 1
+        fetch(c + 2);
+        const uint32_t keys = smem_u32(smem) + (c % kStages) * kStage, head = keys + kKeyBytes;
+        const DeltaFactors& F = *reinterpret_cast<const DeltaFactors*>(smem + (c % kStages) * kStage + kKeyBytes + kFactors);
+        float zero = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) zero = fmaf(v[i][k], 0.f, zero);
+        if (__any_sync(0xffffffffu, F.irregular || zero != 0.f)) {
+            walk_chunk_tokens<T, DKP>(a, S, h, hk, col0, t0 + (long long)c * kChunk, (int)min((long long)kChunk, t1 - t0 - (long long)c * kChunk));
+            values(c + 1);
+            continue;
+        }
+        // S^T k and S^T q
+        float m0 = 0.f, m1 = 0.f, back0, back1;
+#pragma unroll
+        for (int j = 0; j < DKP / 8; ++j) {
+            m0 = fmaxf(m0, fmaxf(fabsf(S[j][0]), fabsf(S[j][1])));
+            m1 = fmaxf(m1, fmaxf(fabsf(S[j][2]), fabsf(S[j][3])));
+        }
+        const float by0 = scale_of<13>(quad_max(m0), back0), by1 = scale_of<13>(quad_max(m1), back1);
+        float r[4][4] = {}, o[4][4] = {};
+#pragma unroll
+        for (int j = 0; j < DKP / 16; ++j) {
+            uint32_t hi[4], lo[4], b[2][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float* p = &S[2 * j + (i >> 1)][(i & 1) * 2];
+                split_pair(p[0] * (i & 1 ? by1 : by0), p[1] * (i & 1 ? by1 : by0), hi[i], lo[i]);
+            }
+            const uint32_t at = keys + (row_at ^ (32 * j));
+            load_matrices(b[0], at);
+            load_matrices(b[1], at + kRows / 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(r[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(r[i], lo, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+            load_matrices(b[0], at + kRows);
+            load_matrices(b[1], at + kRows + kRows / 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(o[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(o[i], lo, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+            if (LO) {
+                load_matrices(b[0], at + 2 * kRows);
+                load_matrices(b[1], at + 2 * kRows + kRows / 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mma_f16(r[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+                load_matrices(b[0], at + 3 * kRows);
+                load_matrices(b[1], at + 3 * kRows + kRows / 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mma_f16(o[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+            }
+        }
+        // what the tokens bring, less what the state holds for their keys
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 put = *reinterpret_cast<const float2*>(&F.put[8 * i + 2 * t]), keep = *reinterpret_cast<const float2*>(&F.keep[8 * i + 2 * t]);
+            const float2 fs = *reinterpret_cast<const float2*>(&F.from_state[8 * i + 2 * t]);
+            v[i][0] = fmaf(-keep.x, r[i][0] * back0, put.x * v[i][0]);
+            v[i][1] = fmaf(-keep.y, r[i][1] * back0, put.y * v[i][1]);
+            v[i][2] = fmaf(-keep.x, r[i][2] * back1, put.x * v[i][2]);
+            v[i][3] = fmaf(-keep.y, r[i][3] * back1, put.y * v[i][3]);
+            o[i][0] *= fs.x * back0; o[i][1] *= fs.y * back0; o[i][2] *= fs.x * back1; o[i][3] *= fs.y * back1;
+        }
+        uint32_t hi[2][4], lo[2][4];
+        float x[4][4] = {};
+        rows_max(v, m0, m1);
+        {
+            const float s0 = scale_of<13>(m0, back0), s1 = scale_of<13>(m1, back1);
+            split_tile(v, s0, s1, hi, lo);
+        }
+        values(c + 1);
+        times_lower(x, hi, lo, head + kSolveHi + mat_at, kSolveLo - kSolveHi);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[i][0] *= back0; x[i][1] *= back0; x[i][2] *= back1; x[i][3] *= back1; }
+        // the chunk's own part of the outputs
+        rows_max(x, m0, m1);
+        {
+            const float s0 = scale_of<13>(m0, back0), s1 = scale_of<13>(m1, back1);
+            split_tile(x, s0, s1, hi, lo);
+        }
+        float inner[4][4] = {};
+        times_lower(inner, hi, lo, head + kInnerHi + mat_at, kInnerLo - kInnerHi);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 fc = *reinterpret_cast<const float2*>(&F.from_chunk[8 * i + 2 * t]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float out = fmaf(inner[i][k], (k & 1 ? fc.y : fc.x) * (k >> 1 ? back1 : back0), o[i][k]);
+                const long long at = t0 + (long long)c * kChunk + 8 * i + 2 * t + (k & 1);
+                const int col = col0 + g + (k >> 1) * 8;
+                if (at < t1 && col < a.v_dim) static_cast<T*>(a.o)[at * a.ldo + (long long)h * a.v_dim + col] = from_float<T>(out);
+            }
+        }
+        // the state behind the chunk
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 te = *reinterpret_cast<const float2*>(&F.to_end[8 * i + 2 * t]);
+            x[i][0] *= te.x; x[i][1] *= te.y; x[i][2] *= te.x; x[i][3] *= te.y;
+        }
+        rows_max(x, m0, m1);
+        {
+            const float s0 = scale_of<13>(m0, back0), s1 = scale_of<13>(m1, back1);
+            split_tile(x, s0, s1, hi, lo);
+        }
+        const float whole = F.whole;
+#pragma unroll
+        for (int j = 0; j < DKP / 8; ++j) {
+            float add[4] = {};
+            uint32_t b[4];
+            load_matrices_transposed(b, keys + (row_at_t ^ (16 * j)));
+            mma_f16(add, lo[0], b[0], b[1]);
+            mma_f16(add, lo[1], b[2], b[3]);
+            if (LO) {
+                uint32_t bl[4];
+                load_matrices_transposed(bl, keys + (row_at_t ^ (16 * j)) + 2 * kRows);
+                mma_f16(add, hi[0], bl[0], bl[1]);
+                mma_f16(add, hi[1], bl[2], bl[3]);
+            }
+            mma_f16(add, hi[0], b[0], b[1]);
+            mma_f16(add, hi[1], b[2], b[3]);
+            S[j][0] = fmaf(add[0], back0, whole * S[j][0]);
+            S[j][1] = fmaf(add[1], back0, whole * S[j][1]);
+            S[j][2] = fmaf(add[2], back1, whole * S[j][2]);
+            S[j][3] = fmaf(add[3], back1, whole * S[j][3]);
+        }
+    }
+    copies_wait<0>();
+    if (slot < 0) return;
+#pragma unroll
+    for (int j = 0; j < DKP / 8; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 8 * j + 2 * t + (i & 1), col = col0 + g + (i >> 1) * 8;
+            if (r < a.k_dim && col < a.v_dim) home[(long long)r * a.v_dim + col] = S[j][i];
+        }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------
+
+#define CSB_CUDA(call)                                                                     \
+    do {                                                                                   \
+        cudaError_t e_ = (call);                                                           \
+        if (e_ != cudaSuccess) {                                                           \
+            set_error("%s failed: %s", #call, cudaGetErrorString(e_));                     \
+            return e_ == cudaErrorMemoryAllocation ? CSB_ERR_ALLOC : CSB_ERR_CUDA;         \
+        }                                                                                  \
+    } while (0)
+
+static int padded(int k_dim) { return k_dim <= 64 ? 64 : k_dim <= 128 ? 128 : 256; }
+static int key_bytes(int k_dim, int dtype) { return (dtype == CSB_F32 ? 4 : 2) * kChunk * padded(k_dim) * 2; }
+
+int64_t delta_chunk_bytes(int64_t tokens, int64_t sequences, int k_heads, int v_heads, int k_dim, int dtype) {
+    return (tokens / kChunk + sequences) * ((int64_t)k_heads * key_bytes(k_dim, dtype) + (int64_t)v_heads * kHeadBytes);
+}
+
+template <typename T, int DKP>
+static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
+    DeltaChunkArgs w{};
+    w.records = a.tokens / kChunk + a.sequences;
+    w.key_bytes = key_bytes(DKP, sizeof(T) == 4 ? CSB_F32 : CSB_F16);
+    w.keys = static_cast<uint8_t*>(workspace);
+    w.heads = w.keys + w.records * a.k_heads * (int64_t)w.key_bytes;
+    // warps of a CTA share a head's records: as many as leave no SM without a CTA
+    const int tiles = (a.v_dim + 15) / 16;
+    w.tiles_a_cta = std::min(tiles, 8);
+    while (w.tiles_a_cta > 2 && (int64_t)a.sequences * a.v_heads * ((tiles + w.tiles_a_cta - 1) / w.tiles_a_cta) < 148) w.tiles_a_cta = (w.tiles_a_cta + 1) / 2;
+    w.groups = (tiles + w.tiles_a_cta - 1) / w.tiles_a_cta;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.stream = (cudaStream_t)stream; cfg.attrs = attr; cfg.numAttrs = 1;
+    cfg.gridDim = dim3((unsigned)w.records, (unsigned)a.k_heads); cfg.blockDim = dim3(kPrepareWarps * 32);
+    cfg.dynamicSmemBytes = sizeof(PrepareSmem<DKP, sizeof(T) == 4>);
+    CSB_CUDA((cudaFuncSetAttribute(csb_delta_prepare_kernel<T, DKP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
+    CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_prepare_kernel<T, DKP>, a, w)));
+    cfg.gridDim = dim3((unsigned)((int64_t)a.sequences * a.v_heads * w.groups)); cfg.blockDim = dim3((unsigned)w.tiles_a_cta * 32);
+    cfg.dynamicSmemBytes = kStages * stage_bytes<T, DKP>();
+    CSB_CUDA((cudaFuncSetAttribute(csb_delta_chunk_kernel<T, DKP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
+    CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_chunk_kernel<T, DKP>, a, w)));
+    return CSB_OK;
+}
+
+template <typename T>
+static int launch_chunks_of(const DeltaArgs& a, void* workspace, void* stream) {
+    const int dkp = padded(a.k_dim);
+    return dkp == 64 ? launch_chunks<T, 64>(a, workspace, stream) : dkp == 128 ? launch_chunks<T, 128>(a, workspace, stream) : launch_chunks<T, 256>(a, workspace, stream);
+}
+
+int launch_delta_chunks(int dtype, const DeltaArgs& a, void* workspace, void* stream) {
+    return dtype == CSB_F32 ? launch_chunks_of<float>(a, workspace, stream) : dtype == CSB_F16 ? launch_chunks_of<__half>(a, workspace, stream)
+                                                                                          : launch_chunks_of<__nv_bfloat16>(a, workspace, stream);
+}
+
+}  // namespace csb
