@@ -255,8 +255,9 @@ __global__ void __launch_bounds__(kPrepareWarps * 32) csb_delta_prepare_kernel(c
 
 // ---------------------------------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ void copy_16(uint32_t to, const void* from) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+// 16 bytes to shared memory, the first `bytes` of them from `from` and zeros behind.
+__device__ __forceinline__ void copy_16(uint32_t to, const void* from, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -318,7 +319,8 @@ __device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)
         const T *kp = static_cast<const T*>(a.k) + (long long)hk * a.k_dim + at * a.ldk, *qp = static_cast<const T*>(a.q) + (long long)hk * a.k_dim + at * a.ldq;
         float kk = 0.f, qq = 0.f, dot = 0.f, u[2] = {0.f, 0.f}, o[2] = {0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < DKP / 8; ++j)
+        for (int j = 0; j < DKP / 8; ++j) {
+            if (j % 4 == 0) asm volatile("" ::: "memory");       // (few loads in flight, few registers: the path is rare)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int c = 8 * j + 2 * t + e;
@@ -328,20 +330,22 @@ __device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)
                 u[0] = fmaf(x, S[j][e], u[0]); u[1] = fmaf(x, S[j][2 + e], u[1]);
                 o[0] = fmaf(y, S[j][e], o[0]); o[1] = fmaf(y, S[j][2 + e], o[1]);
             }
+        }
         kk = quad_sum(kk); qq = quad_sum(qq); dot = quad_sum(dot);
         const float kn = a.normalize ? 1.f / sqrtf(kk + kDeltaEps) : 1.f, qn = a.scale * (a.normalize ? 1.f / sqrtf(qq + kDeltaEps) : 1.f);
         const float decay = expf(a.g[at * a.ldg + h]), beta = a.beta[at * a.ldb + h];
         float add[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const int col = col0 + (lane >> 2) + 8 * r;
+            const int col = col0 + 2 * (lane >> 2) + r;
             const float seen = decay * kn * quad_sum(u[r]), old = decay * quad_sum(o[r]);
             const float v = col < a.v_dim ? to_float(static_cast<const T*>(a.v)[at * a.ldv + (long long)h * a.v_dim + col]) : 0.f;
             add[r] = kn * (beta * (v - seen));
             if (t == 0 && col < a.v_dim) static_cast<T*>(a.o)[at * a.ldo + (long long)h * a.v_dim + col] = from_float<T>(qn * (old + dot * add[r]));
         }
 #pragma unroll
-        for (int j = 0; j < DKP / 8; ++j)
+        for (int j = 0; j < DKP / 8; ++j) {
+            if (j % 4 == 0) asm volatile("" ::: "memory");
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int c = 8 * j + 2 * t + e;
@@ -350,17 +354,21 @@ __device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)
                 S[j][e] = fmaf(x, add[0], decay * S[j][e]);
                 S[j][2 + e] = fmaf(x, add[1], decay * S[j][2 + e]);
             }
+        }
     }
 }
 
-template <typename T, int DKP>
-__host__ __device__ constexpr int stage_bytes() { return (sizeof(T) == 4 ? 4 : 2) * kChunk * DKP * 2 + kHeadBytes; }
-constexpr int kStages = 3;
+// Two neighbouring values.
+__device__ __forceinline__ float2 load_pair(const float* p) { return *reinterpret_cast<const float2*>(p); }
+template <typename T> __device__ __forceinline__ float2 load_pair(const T* p) { return pair_to_float(*reinterpret_cast<const uint32_t*>(p), T()); }
+__device__ __forceinline__ void store_pair(float* p, float x, float y) { *reinterpret_cast<float2*>(p) = make_float2(x, y); }
+__device__ __forceinline__ void store_pair(__half* p, float x, float y) { *reinterpret_cast<__half2*>(p) = __floats2half2_rn(x, y); }
+__device__ __forceinline__ void store_pair(__nv_bfloat16* p, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y); }
 
 template <typename T, int DKP>
-__global__ void __launch_bounds__(256) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
+__global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
     constexpr bool LO = sizeof(T) == 4;
-    constexpr int kStage = stage_bytes<T, DKP>(), kRows = kChunk * DKP * 2;
+    constexpr int kRows = kChunk * DKP * 2;
     constexpr int kKeyBytes = (LO ? 4 : 2) * kRows;
     extern __shared__ __align__(512) uint8_t smem[];
     pdl_launch_dependents();
@@ -376,7 +384,8 @@ __global__ void __launch_bounds__(256) csb_delta_chunk_kernel(const DeltaArgs a,
         if (slot < 0) return;
     }
     if (t0 >= t1) return;
-    const int col0 = (group * w.tiles_a_cta + warp) * 16;       // (a warp behind the last column works on zeros)
+    // Rows g and g + 8 of a tile, which a lane has, are neighbouring columns of the head.  (A warp behind the last column works on zeros.)
+    const int col0 = (group * w.tiles_a_cta + warp) * 16;
     float S[DKP / 8][4];
     float* home = a.state + ((slot < 0 ? 0 : slot) * a.v_heads + h) * (long long)a.k_dim * a.v_dim;
     const bool from_zero = slot < 0 || (a.fresh && a.fresh[seq]);
@@ -384,54 +393,68 @@ __global__ void __launch_bounds__(256) csb_delta_chunk_kernel(const DeltaArgs a,
     for (int j = 0; j < DKP / 8; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = 8 * j + 2 * t + (i & 1), col = col0 + g + (i >> 1) * 8;
+            const int r = 8 * j + 2 * t + (i & 1), col = col0 + 2 * g + (i >> 1);
             S[j][i] = !from_zero && r < a.k_dim && col < a.v_dim ? home[(long long)r * a.v_dim + col] : 0.f;
         }
 
-    const int chunks = (int)((t1 - t0 + kChunk - 1) / kChunk);
+    const int tokens = (int)(t1 - t0), chunks = (tokens + kChunk - 1) / kChunk;
     const long long rec0 = t0 / kChunk + seq;
+    // Chunk c's records and its values of the CTA's columns (zeros where there are none), the next free stage.
+    const int first_col = group * w.tiles_a_cta * 16, values_a_row = w.tiles_a_cta * 16, pitch = values_a_row * (int)sizeof(T) + 16;
+    const T* vp = static_cast<const T*>(a.v) + t0 * a.ldv + (long long)h * a.v_dim + first_col;
+    int put_stage = 0;
     auto fetch = [&](int c) {
         if (c < chunks) {
-            const uint32_t to = smem_u32(smem) + (c % kStages) * kStage;
+            const uint32_t to = smem_u32(smem) + put_stage * w.stage_bytes;
             const uint8_t *keys = w.keys + ((rec0 + c) * a.k_heads + hk) * w.key_bytes, *head = w.heads + ((rec0 + c) * a.v_heads + h) * kHeadBytes;
-            for (int i = threadIdx.x * 16; i < kKeyBytes; i += blockDim.x * 16) copy_16(to + i, keys + i);
-            for (int i = threadIdx.x * 16; i < kFactors + (int)sizeof(DeltaFactors); i += blockDim.x * 16) copy_16(to + kKeyBytes + i, head + i);
+            for (int i = threadIdx.x * 16; i < kKeyBytes; i += blockDim.x * 16) copy_16(to + i, keys + i, 16);
+            for (int i = threadIdx.x * 16; i < kFactors + (int)sizeof(DeltaFactors); i += blockDim.x * 16) copy_16(to + kKeyBytes + i, head + i, 16);
+            constexpr int kUnit = 16 / (int)sizeof(T);
+            if (w.values_async) {
+                const int units = values_a_row / kUnit;         // of a row
+                for (int i = threadIdx.x; i < kChunk * units; i += blockDim.x) {
+                    const int at = c * kChunk + i / units, u = i % units * kUnit;
+                    const bool there = at < tokens && first_col + u < a.v_dim;
+                    copy_16(to + kKeyBytes + kHeadBytes + (i / units) * pitch + u * (int)sizeof(T), there ? vp + at * a.ldv + u : vp, there ? 16 : 0);
+                }
+            } else {
+                T* out = reinterpret_cast<T*>(smem + put_stage * w.stage_bytes + kKeyBytes + kHeadBytes);
+                for (int i = threadIdx.x; i < kChunk * values_a_row; i += blockDim.x) {
+                    const int at = c * kChunk + i / values_a_row, u = i % values_a_row;
+                    out[(i / values_a_row) * (pitch / (int)sizeof(T)) + u] = at < tokens && first_col + u < a.v_dim ? vp[at * a.ldv + u] : from_float<T>(0.f);
+                }
+            }
         }
         copies_commit();
+        if (++put_stage == w.stages) put_stage = 0;
     };
-    // values of this lane's columns g, g + 8 for its tokens 8i + 2t, 8i + 2t + 1
-    float v[4][4];
-    auto values = [&](int c) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const long long at = t0 + (long long)c * kChunk + 8 * i + 2 * t + (k & 1);
-                const int col = col0 + g + (k >> 1) * 8;
-                v[i][k] = at < t1 && col < a.v_dim ? to_float(static_cast<const T*>(a.v)[at * a.ldv + (long long)h * a.v_dim + col]) : 0.f;
-            }
-    };
+    const int col = col0 + 2 * g;                               // this lane's first column
+    const bool pairs = w.pairs && col + 1 < a.v_dim;
+    T* op = static_cast<T*>(a.o) + t0 * a.ldo + (long long)h * a.v_dim + col;
     fetch(0);
-    fetch(1);
-    values(0);
+    if (w.stages == 3) fetch(1);
     // this lane's places in the operands (see load_matrices): rows are tokens, units 32 bytes a step apart
     const int tok = (lane >> 4) * 8 + (lane & 7);
     const uint32_t row_at = tok * DKP * 2 + (((lane >> 3 & 1) ^ (tok & 7)) << 4), row_at_t = lane * DKP * 2 + ((lane & 7) << 4);
     const uint32_t mat_at = matrix_at(tok, (lane >> 3 & 1) * 8);
-    for (int c = 0; c < chunks; ++c) {
-        copies_wait<1>();
+    for (int c = 0, stage = 0; c < chunks; ++c) {
+        if (w.stages == 3) copies_wait<1>(); else copies_wait<0>();
         __syncthreads();                                        // chunk c is there, and everybody is done with chunk c - 1
-        fetch(c + 2);
-        const uint32_t keys = smem_u32(smem) + (c % kStages) * kStage, head = keys + kKeyBytes;
-        const DeltaFactors& F = *reinterpret_cast<const DeltaFactors*>(smem + (c % kStages) * kStage + kKeyBytes + kFactors);
-        float zero = 0.f;
+        fetch(c + w.stages - 1);
+        const uint8_t* here = smem + stage * w.stage_bytes;
+        const uint32_t keys = smem_u32(here), head = keys + kKeyBytes;
+        const DeltaFactors& F = *reinterpret_cast<const DeltaFactors*>(here + kKeyBytes + kFactors);
+        const uint8_t* mine = here + kKeyBytes + kHeadBytes + (warp * 16 + 2 * g) * (int)sizeof(T) + 2 * t * pitch;
+        if (++stage == w.stages) stage = 0;
+        float v[4][4], zero = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) zero = fmaf(v[i][k], 0.f, zero);
+        for (int i = 0; i < 8; ++i) {
+            const float2 f = load_pair(reinterpret_cast<const T*>(mine + (8 * (i >> 1) + (i & 1)) * pitch));
+            v[i >> 1][i & 1] = f.x; v[i >> 1][2 + (i & 1)] = f.y;
+            zero = fmaf(f.x, 0.f, fmaf(f.y, 0.f, zero));
+        }
         if (__any_sync(0xffffffffu, F.irregular || zero != 0.f)) {
-            walk_chunk_tokens<T, DKP>(a, S, h, hk, col0, t0 + (long long)c * kChunk, (int)min((long long)kChunk, t1 - t0 - (long long)c * kChunk));
-            values(c + 1);
+            walk_chunk_tokens<T, DKP>(a, S, h, hk, col0, t0 + (long long)c * kChunk, min(kChunk, tokens - c * kChunk));
             continue;
         }
         // S^T k and S^T q
@@ -493,7 +516,6 @@ __global__ void __launch_bounds__(256) csb_delta_chunk_kernel(const DeltaArgs a,
             const float s0 = scale_of<13>(m0, back0), s1 = scale_of<13>(m1, back1);
             split_tile(v, s0, s1, hi, lo);
         }
-        values(c + 1);
         times_lower(x, hi, lo, head + kSolveHi + mat_at, kSolveLo - kSolveHi);
 #pragma unroll
         for (int i = 0; i < 4; ++i) { x[i][0] *= back0; x[i][1] *= back0; x[i][2] *= back1; x[i][3] *= back1; }
@@ -509,11 +531,17 @@ __global__ void __launch_bounds__(256) csb_delta_chunk_kernel(const DeltaArgs a,
         for (int i = 0; i < 4; ++i) {
             const float2 fc = *reinterpret_cast<const float2*>(&F.from_chunk[8 * i + 2 * t]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float out = fmaf(inner[i][k], (k & 1 ? fc.y : fc.x) * (k >> 1 ? back1 : back0), o[i][k]);
-                const long long at = t0 + (long long)c * kChunk + 8 * i + 2 * t + (k & 1);
-                const int col = col0 + g + (k >> 1) * 8;
-                if (at < t1 && col < a.v_dim) static_cast<T*>(a.o)[at * a.ldo + (long long)h * a.v_dim + col] = from_float<T>(out);
+            for (int k = 0; k < 2; ++k) {
+                const float f = k ? fc.y : fc.x, x0 = fmaf(inner[i][k], f * back0, o[i][k]), x1 = fmaf(inner[i][2 + k], f * back1, o[i][2 + k]);
+                const int at = c * kChunk + 8 * i + 2 * t + k;
+                T* p = op + at * a.ldo;
+                if (at < tokens) {
+                    if (pairs) store_pair(p, x0, x1);
+                    else if (col < a.v_dim) {
+                        p[0] = from_float<T>(x0);
+                        if (col + 1 < a.v_dim) p[1] = from_float<T>(x1);
+                    }
+                }
             }
         }
         // the state behind the chunk
@@ -555,7 +583,7 @@ __global__ void __launch_bounds__(256) csb_delta_chunk_kernel(const DeltaArgs a,
     for (int j = 0; j < DKP / 8; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = 8 * j + 2 * t + (i & 1), col = col0 + g + (i >> 1) * 8;
+            const int r = 8 * j + 2 * t + (i & 1), col = col0 + 2 * g + (i >> 1);
             if (r < a.k_dim && col < a.v_dim) home[(long long)r * a.v_dim + col] = S[j][i];
         }
 }
@@ -590,6 +618,10 @@ static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
     w.tiles_a_cta = std::min(tiles, 8);
     while (w.tiles_a_cta > 2 && (int64_t)a.sequences * a.v_heads * ((tiles + w.tiles_a_cta - 1) / w.tiles_a_cta) < 148) w.tiles_a_cta = (w.tiles_a_cta + 1) / 2;
     w.groups = (tiles + w.tiles_a_cta - 1) / w.tiles_a_cta;
+    w.pairs = a.v_dim % 2 == 0 && a.ldo % 2 == 0 && reinterpret_cast<uintptr_t>(a.o) % (2 * sizeof(T)) == 0;
+    w.values_async = a.v_dim * sizeof(T) % 16 == 0 && a.ldv * sizeof(T) % 16 == 0 && reinterpret_cast<uintptr_t>(a.v) % 16 == 0;
+    w.stage_bytes = w.key_bytes + kHeadBytes + kChunk * (w.tiles_a_cta * 16 * (int)sizeof(T) + 16);
+    w.stages = 3 * w.stage_bytes <= 227 * 1024 ? 3 : 2;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -600,7 +632,7 @@ static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
     CSB_CUDA((cudaFuncSetAttribute(csb_delta_prepare_kernel<T, DKP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
     CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_prepare_kernel<T, DKP>, a, w)));
     cfg.gridDim = dim3((unsigned)((int64_t)a.sequences * a.v_heads * w.groups)); cfg.blockDim = dim3((unsigned)w.tiles_a_cta * 32);
-    cfg.dynamicSmemBytes = kStages * stage_bytes<T, DKP>();
+    cfg.dynamicSmemBytes = (size_t)w.stages * w.stage_bytes;
     CSB_CUDA((cudaFuncSetAttribute(csb_delta_chunk_kernel<T, DKP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
     CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_chunk_kernel<T, DKP>, a, w)));
     return CSB_OK;
