@@ -28,9 +28,8 @@ constexpr int kChunk = 32;
 struct DeltaChunkArgs {
     uint8_t *keys, *heads;              // [records][k_heads] operands of a chunk, [records][v_heads] its matrices and factors
     long long records;
-    int key_bytes, tiles_a_cta, groups; // of a key record; tiles of 16 value columns of a CTA, CTAs of a head
+    int key_bytes, groups;              // of a key record; CTAs of a head
     int pairs, values_async;            // whether two neighbouring outputs are one access; whether v is copied 16 bytes at a time
-    int stages, stage_bytes;            // of shared memory: the records and values of a chunk
 };
 
 // csb_delta_chunk.cu

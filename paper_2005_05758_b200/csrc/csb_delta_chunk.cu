@@ -81,7 +81,6 @@ __global__ void __launch_bounds__(kPrepareWarps * 32) csb_delta_prepare_kernel(c
     constexpr bool LO = sizeof(T) == 4;
     extern __shared__ __align__(512) uint8_t raw[];
     PrepareSmem<DKP, LO>& M = *reinterpret_cast<PrepareSmem<DKP, LO>*>(raw);
-    pdl_launch_dependents();
     pdl_wait();
     const long long rec = blockIdx.x;
     const int hk = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -282,33 +281,38 @@ __device__ __forceinline__ void split_tile(const float (&x)[4][4], float by0, fl
             split_pair(p[0] * by, p[1] * by, hi[s][i], lo[s][i]);
         }
 }
-__device__ __forceinline__ void rows_max(const float (&x)[4][4], float& m0, float& m1) {
-    m0 = m1 = 0.f;
+// The same, each row's largest value taken to 2^13; the inverse scales of rows g and g + 8.
+__device__ __forceinline__ void split_rows(const float (&x)[4][4], uint32_t (&hi)[2][4], uint32_t (&lo)[2][4], float& inv0, float& inv1) {
+    float m0 = 0.f, m1 = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         m0 = fmaxf(m0, fmaxf(fabsf(x[i][0]), fabsf(x[i][1])));
         m1 = fmaxf(m1, fmaxf(fabsf(x[i][2]), fabsf(x[i][3])));
     }
-    m0 = quad_max(m0); m1 = quad_max(m1);
+    const float by0 = scale_of<13>(quad_max(m0), inv0), by1 = scale_of<13>(quad_max(m1), inv1);
+    split_tile(x, by0, by1, hi, lo);
+}
+// What takes a largest value into [2^8, 2^9), for a row that is divided by `back` to get its true values' scale (which stays below 2^100).
+__device__ __forceinline__ float settled(float largest, float back) {
+    float inverse;
+    const float f = scale_of<8>(largest, inverse);
+    return largest > 0.f ? fminf(f, 0x1p100f * back) : 1.f;
 }
 // d += x M^T for a 32 x 32 matrix without an upper part; `at` is this lane's place in it, `lo` where its second half lies.
 // (The product of the two second halves is left out: 2^-22.)
 __device__ __forceinline__ void times_lower(float (&d)[4][4], const uint32_t (&hi)[2][4], const uint32_t (&lo)[2][4], uint32_t at, uint32_t lo_at) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 2; ++s) {                               // (tiles in turn: a product waits for the one before it on its tile)
+        uint32_t b[2][4], l[2][4];
 #pragma unroll
-        for (int p = s; p < 2; ++p) {
-            uint32_t b[4];
-            load_matrices(b, (at ^ (32 * s)) + p * 16 * 64);
+        for (int p = s; p < 2; ++p) { load_matrices(b[p], (at ^ (32 * s)) + p * 16 * 64); load_matrices(l[p], (at ^ (32 * s)) + p * 16 * 64 + lo_at); }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                mma_f16(d[2 * p + i], hi[s], b[2 * i], b[2 * i + 1]);
-                mma_f16(d[2 * p + i], lo[s], b[2 * i], b[2 * i + 1]);
-            }
-            load_matrices(b, (at ^ (32 * s)) + p * 16 * 64 + lo_at);
+        for (int i = 2 * s; i < 4; ++i) mma_f16(d[i], lo[s], b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) mma_f16(d[2 * p + i], hi[s], b[2 * i], b[2 * i + 1]);
-        }
+        for (int i = 2 * s; i < 4; ++i) mma_f16(d[i], hi[s], l[i >> 1][(i & 1) * 2], l[i >> 1][(i & 1) * 2 + 1]);
+#pragma unroll
+        for (int i = 2 * s; i < 4; ++i) mma_f16(d[i], hi[s], b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+    }
 }
 
 // Tokens [first, first + n) one by one in fp32 on a warp's part of the state.
@@ -365,11 +369,18 @@ __device__ __forceinline__ void store_pair(float* p, float x, float y) { *reinte
 __device__ __forceinline__ void store_pair(__half* p, float x, float y) { *reinterpret_cast<__half2*>(p) = __floats2half2_rn(x, y); }
 __device__ __forceinline__ void store_pair(__nv_bfloat16* p, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y); }
 
-template <typename T, int DKP>
-__global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
+// Shared memory of a chunk: the records and the values of W tiles.  Three chunks where they fit, else two.
+template <typename T, int DKP, int W>
+__host__ __device__ constexpr int stage_bytes() { return (sizeof(T) == 4 ? 4 : 2) * kChunk * DKP * 2 + kHeadBytes + kChunk * (W * 16 * (int)sizeof(T) + 16); }
+template <typename T, int DKP, int W>
+__host__ __device__ constexpr int stage_count() { return 3 * stage_bytes<T, DKP, W>() <= 227 * 1024 ? 3 : 2; }
+
+template <typename T, int DKP, int W>
+__global__ void __launch_bounds__(W * 32, 1) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
     constexpr bool LO = sizeof(T) == 4;
     constexpr int kRows = kChunk * DKP * 2;
     constexpr int kKeyBytes = (LO ? 4 : 2) * kRows;
+    constexpr int kStage = stage_bytes<T, DKP, W>(), kStages = stage_count<T, DKP, W>();
     extern __shared__ __align__(512) uint8_t smem[];
     pdl_launch_dependents();
     pdl_wait();
@@ -385,7 +396,7 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
     }
     if (t0 >= t1) return;
     // Rows g and g + 8 of a tile, which a lane has, are neighbouring columns of the head.  (A warp behind the last column works on zeros.)
-    const int col0 = (group * w.tiles_a_cta + warp) * 16;
+    const int col0 = (group * W + warp) * 16;
     float S[DKP / 8][4];
     float* home = a.state + ((slot < 0 ? 0 : slot) * a.v_heads + h) * (long long)a.k_dim * a.v_dim;
     const bool from_zero = slot < 0 || (a.fresh && a.fresh[seq]);
@@ -396,75 +407,99 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
             const int r = 8 * j + 2 * t + (i & 1), col = col0 + 2 * g + (i >> 1);
             S[j][i] = !from_zero && r < a.k_dim && col < a.v_dim ? home[(long long)r * a.v_dim + col] : 0.f;
         }
-
-    const int tokens = (int)(t1 - t0), chunks = (tokens + kChunk - 1) / kChunk;
-    const long long rec0 = t0 / kChunk + seq;
-    // Chunk c's records and its values of the CTA's columns (zeros where there are none), the next free stage.
-    const int first_col = group * w.tiles_a_cta * 16, values_a_row = w.tiles_a_cta * 16, pitch = values_a_row * (int)sizeof(T) + 16;
-    const T* vp = static_cast<const T*>(a.v) + t0 * a.ldv + (long long)h * a.v_dim + first_col;
-    int put_stage = 0;
-    auto fetch = [&](int c) {
-        if (c < chunks) {
-            const uint32_t to = smem_u32(smem) + put_stage * w.stage_bytes;
-            const uint8_t *keys = w.keys + ((rec0 + c) * a.k_heads + hk) * w.key_bytes, *head = w.heads + ((rec0 + c) * a.v_heads + h) * kHeadBytes;
-            for (int i = threadIdx.x * 16; i < kKeyBytes; i += blockDim.x * 16) copy_16(to + i, keys + i, 16);
-            for (int i = threadIdx.x * 16; i < kFactors + (int)sizeof(DeltaFactors); i += blockDim.x * 16) copy_16(to + kKeyBytes + i, head + i, 16);
-            constexpr int kUnit = 16 / (int)sizeof(T);
-            if (w.values_async) {
-                const int units = values_a_row / kUnit;         // of a row
-                for (int i = threadIdx.x; i < kChunk * units; i += blockDim.x) {
-                    const int at = c * kChunk + i / units, u = i % units * kUnit;
-                    const bool there = at < tokens && first_col + u < a.v_dim;
-                    copy_16(to + kKeyBytes + kHeadBytes + (i / units) * pitch + u * (int)sizeof(T), there ? vp + at * a.ldv + u : vp, there ? 16 : 0);
-                }
-            } else {
-                T* out = reinterpret_cast<T*>(smem + put_stage * w.stage_bytes + kKeyBytes + kHeadBytes);
-                for (int i = threadIdx.x; i < kChunk * values_a_row; i += blockDim.x) {
-                    const int at = c * kChunk + i / values_a_row, u = i % values_a_row;
-                    out[(i / values_a_row) * (pitch / (int)sizeof(T)) + u] = at < tokens && first_col + u < a.v_dim ? vp[at * a.ldv + u] : from_float<T>(0.f);
-                }
-            }
-        }
-        copies_commit();
-        if (++put_stage == w.stages) put_stage = 0;
-    };
-    const int col = col0 + 2 * g;                               // this lane's first column
-    const bool pairs = w.pairs && col + 1 < a.v_dim;
-    T* op = static_cast<T*>(a.o) + t0 * a.ldo + (long long)h * a.v_dim + col;
-    fetch(0);
-    if (w.stages == 3) fetch(1);
-    // this lane's places in the operands (see load_matrices): rows are tokens, units 32 bytes a step apart
-    const int tok = (lane >> 4) * 8 + (lane & 7);
-    const uint32_t row_at = tok * DKP * 2 + (((lane >> 3 & 1) ^ (tok & 7)) << 4), row_at_t = lane * DKP * 2 + ((lane & 7) << 4);
-    const uint32_t mat_at = matrix_at(tok, (lane >> 3 & 1) * 8);
-    for (int c = 0, stage = 0; c < chunks; ++c) {
-        if (w.stages == 3) copies_wait<1>(); else copies_wait<0>();
-        __syncthreads();                                        // chunk c is there, and everybody is done with chunk c - 1
-        fetch(c + w.stages - 1);
-        const uint8_t* here = smem + stage * w.stage_bytes;
-        const uint32_t keys = smem_u32(here), head = keys + kKeyBytes;
-        const DeltaFactors& F = *reinterpret_cast<const DeltaFactors*>(here + kKeyBytes + kFactors);
-        const uint8_t* mine = here + kKeyBytes + kHeadBytes + (warp * 16 + 2 * g) * (int)sizeof(T) + 2 * t * pitch;
-        if (++stage == w.stages) stage = 0;
-        float v[4][4], zero = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 f = load_pair(reinterpret_cast<const T*>(mine + (8 * (i >> 1) + (i & 1)) * pitch));
-            v[i >> 1][i & 1] = f.x; v[i >> 1][2 + (i & 1)] = f.y;
-            zero = fmaf(f.x, 0.f, fmaf(f.y, 0.f, zero));
-        }
-        if (__any_sync(0xffffffffu, F.irregular || zero != 0.f)) {
-            walk_chunk_tokens<T, DKP>(a, S, h, hk, col0, t0 + (long long)c * kChunk, min(kChunk, tokens - c * kChunk));
-            continue;
-        }
-        // S^T k and S^T q
-        float m0 = 0.f, m1 = 0.f, back0, back1;
+    // The state is held times a power of two a row (by, its inverse back), such that it fits binary16 with room to
+    // grow: its bound (kept up to date by what every chunk adds at most) stays within 2^4 .. 2^15, and where it leaves that, the
+    // row's largest value is looked up and taken to 2^8.  What a chunk adds, `add` at most in all, is scaled alike.
+    float by0 = 1.f, by1 = 1.f, back0 = 1.f, back1 = 1.f, bound0, bound1;
+    auto settle = [&](float add0, float add1) {
+        float m0 = 0.f, m1 = 0.f;
 #pragma unroll
         for (int j = 0; j < DKP / 8; ++j) {
             m0 = fmaxf(m0, fmaxf(fabsf(S[j][0]), fabsf(S[j][1])));
             m1 = fmaxf(m1, fmaxf(fabsf(S[j][2]), fabsf(S[j][3])));
         }
-        const float by0 = scale_of<13>(quad_max(m0), back0), by1 = scale_of<13>(quad_max(m1), back1);
+        m0 = quad_max(m0); m1 = quad_max(m1);
+        const float f0 = settled(fmaxf(m0, add0), back0), f1 = settled(fmaxf(m1, add1), back1);
+#pragma unroll
+        for (int j = 0; j < DKP / 8; ++j) { S[j][0] *= f0; S[j][1] *= f0; S[j][2] *= f1; S[j][3] *= f1; }
+        by0 *= f0; by1 *= f1; back0 /= f0; back1 /= f1;
+        bound0 = m0 * f0; bound1 = m1 * f1;
+    };
+    settle(0.f, 0.f);
+
+    const int tokens = (int)(t1 - t0), chunks = (tokens + kChunk - 1) / kChunk;
+    const long long rec0 = t0 / kChunk + seq;
+    // Chunk c's records and its values of the CTA's columns (zeros where there are none), the next free stage.
+    const int first_col = group * W * 16;
+    constexpr int kValues = W * 16, kPitch = kValues * (int)sizeof(T) + 16;
+    const T* vp = static_cast<const T*>(a.v) + t0 * a.ldv + (long long)h * a.v_dim + first_col;
+    const uint8_t *keys_at = w.keys + (rec0 * a.k_heads + hk) * w.key_bytes + threadIdx.x * 16;
+    const uint8_t *head_at = w.heads + (rec0 * a.v_heads + h) * kHeadBytes + threadIdx.x * 16;
+    const long long keys_step = (long long)a.k_heads * w.key_bytes, head_step = (long long)a.v_heads * kHeadBytes;
+    constexpr int kUnit = 16 / (int)sizeof(T), kUnits = kValues / kUnit;      // values of 16 bytes, and such of a row
+    constexpr int kHeadUsed = kFactors + (int)sizeof(DeltaFactors);
+    int put_stage = 0;
+    auto fetch = [&](int c) {
+        if (c < chunks) {
+            const uint32_t to = smem_u32(smem) + put_stage * kStage + threadIdx.x * 16;
+#pragma unroll
+            for (int i = 0; i < kKeyBytes; i += W * 512) copy_16(to + i, keys_at + i, 16);
+#pragma unroll
+            for (int i = 0; i < kHeadUsed; i += W * 512)
+                if (i + W * 512 <= kHeadUsed || i + (int)threadIdx.x * 16 < kHeadUsed) copy_16(to + kKeyBytes + i, head_at + i, 16);
+            keys_at += keys_step; head_at += head_step;
+            if (w.values_async) {
+#pragma unroll
+                for (int i = 0; i < kChunk * kUnits; i += W * 32) {
+                    const int row = (i + (int)threadIdx.x) / kUnits, u = (i + (int)threadIdx.x) % kUnits * kUnit, at = c * kChunk + row;
+                    const bool there = at < tokens && first_col + u < a.v_dim;
+                    copy_16(smem_u32(smem) + put_stage * kStage + kKeyBytes + kHeadBytes + row * kPitch + u * (int)sizeof(T), there ? vp + at * a.ldv + u : vp, there ? 16 : 0);
+                }
+            } else {
+                T* out = reinterpret_cast<T*>(smem + put_stage * kStage + kKeyBytes + kHeadBytes);
+                for (int i = threadIdx.x; i < kChunk * kValues; i += W * 32) {
+                    const int at = c * kChunk + i / kValues, u = i % kValues;
+                    out[(i / kValues) * (kPitch / (int)sizeof(T)) + u] = at < tokens && first_col + u < a.v_dim ? vp[at * a.ldv + u] : from_float<T>(0.f);
+                }
+            }
+        }
+        copies_commit();
+        if (++put_stage == kStages) put_stage = 0;
+    };
+    const int col = col0 + 2 * g;                               // this lane's first column
+    const bool pairs = w.pairs && col + 1 < a.v_dim;
+    T* op = static_cast<T*>(a.o) + t0 * a.ldo + (long long)h * a.v_dim + col;
+    fetch(0);
+    if (kStages == 3) fetch(1);
+    // this lane's places in the operands (see load_matrices): rows are tokens, units 32 bytes a step apart
+    const int tok = (lane >> 4) * 8 + (lane & 7);
+    const uint32_t row_at = tok * DKP * 2 + (((lane >> 3 & 1) ^ (tok & 7)) << 4), row_at_t = lane * DKP * 2 + ((lane & 7) << 4);
+    const uint32_t mat_at = matrix_at(tok, (lane >> 3 & 1) * 8);
+    for (int c = 0, stage = 0; c < chunks; ++c) {
+        copies_wait<kStages - 2>();
+        __syncthreads();                                        // chunk c is there, and everybody is done with chunk c - 1
+        fetch(c + kStages - 1);
+        const uint8_t* here = smem + stage * kStage;
+        const uint32_t keys = smem_u32(here), head = keys + kKeyBytes;
+        const DeltaFactors& F = *reinterpret_cast<const DeltaFactors*>(here + kKeyBytes + kFactors);
+        const uint8_t* mine = here + kKeyBytes + kHeadBytes + (warp * 16 + 2 * g) * (int)sizeof(T) + 2 * t * kPitch;
+        if (++stage == kStages) stage = 0;
+        float v[4][4], zero = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 f = load_pair(reinterpret_cast<const T*>(mine + (8 * (i >> 1) + (i & 1)) * kPitch));
+            v[i >> 1][i & 1] = f.x; v[i >> 1][2 + (i & 1)] = f.y;
+            zero = fmaf(f.x, 0.f, fmaf(f.y, 0.f, zero));
+        }
+        if (__any_sync(0xffffffffu, F.irregular || zero != 0.f)) {
+#pragma unroll
+            for (int j = 0; j < DKP / 8; ++j) { S[j][0] *= back0; S[j][1] *= back0; S[j][2] *= back1; S[j][3] *= back1; }
+            by0 = by1 = back0 = back1 = 1.f;
+            walk_chunk_tokens<T, DKP>(a, S, h, hk, col0, t0 + (long long)c * kChunk, min(kChunk, tokens - c * kChunk));
+            settle(0.f, 0.f);
+            continue;
+        }
+        // S^T k and S^T q
         float r[4][4] = {}, o[4][4] = {};
 #pragma unroll
         for (int j = 0; j < DKP / 16; ++j) {
@@ -472,7 +507,7 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float* p = &S[2 * j + (i >> 1)][(i & 1) * 2];
-                split_pair(p[0] * (i & 1 ? by1 : by0), p[1] * (i & 1 ? by1 : by0), hi[i], lo[i]);
+                split_pair(p[0], p[1], hi[i], lo[i]);
             }
             const uint32_t at = keys + (row_at ^ (32 * j));
             load_matrices(b[0], at);
@@ -510,21 +545,13 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
             o[i][0] *= fs.x * back0; o[i][1] *= fs.y * back0; o[i][2] *= fs.x * back1; o[i][3] *= fs.y * back1;
         }
         uint32_t hi[2][4], lo[2][4];
-        float x[4][4] = {};
-        rows_max(v, m0, m1);
-        {
-            const float s0 = scale_of<13>(m0, back0), s1 = scale_of<13>(m1, back1);
-            split_tile(v, s0, s1, hi, lo);
-        }
+        float x[4][4] = {}, inv0, inv1;
+        split_rows(v, hi, lo, inv0, inv1);
         times_lower(x, hi, lo, head + kSolveHi + mat_at, kSolveLo - kSolveHi);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { x[i][0] *= back0; x[i][1] *= back0; x[i][2] *= back1; x[i][3] *= back1; }
+        for (int i = 0; i < 4; ++i) { x[i][0] *= inv0; x[i][1] *= inv0; x[i][2] *= inv1; x[i][3] *= inv1; }
         // the chunk's own part of the outputs
-        rows_max(x, m0, m1);
-        {
-            const float s0 = scale_of<13>(m0, back0), s1 = scale_of<13>(m1, back1);
-            split_tile(x, s0, s1, hi, lo);
-        }
+        split_rows(x, hi, lo, inv0, inv1);
         float inner[4][4] = {};
         times_lower(inner, hi, lo, head + kInnerHi + mat_at, kInnerLo - kInnerHi);
 #pragma unroll
@@ -532,7 +559,7 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
             const float2 fc = *reinterpret_cast<const float2*>(&F.from_chunk[8 * i + 2 * t]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const float f = k ? fc.y : fc.x, x0 = fmaf(inner[i][k], f * back0, o[i][k]), x1 = fmaf(inner[i][2 + k], f * back1, o[i][2 + k]);
+                const float f = k ? fc.y : fc.x, x0 = fmaf(inner[i][k], f * inv0, o[i][k]), x1 = fmaf(inner[i][2 + k], f * inv1, o[i][2 + k]);
                 const int at = c * kChunk + 8 * i + 2 * t + k;
                 T* p = op + at * a.ldo;
                 if (at < tokens) {
@@ -544,37 +571,50 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
                 }
             }
         }
-        // the state behind the chunk
+        // the state behind the chunk (a scaled key's values are below 2)
+        float add0 = 0.f, add1 = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float2 te = *reinterpret_cast<const float2*>(&F.to_end[8 * i + 2 * t]);
             x[i][0] *= te.x; x[i][1] *= te.y; x[i][2] *= te.x; x[i][3] *= te.y;
+            add0 += fabsf(x[i][0]) + fabsf(x[i][1]); add1 += fabsf(x[i][2]) + fabsf(x[i][3]);
         }
-        rows_max(x, m0, m1);
-        {
-            const float s0 = scale_of<13>(m0, back0), s1 = scale_of<13>(m1, back1);
-            split_tile(x, s0, s1, hi, lo);
-        }
+        add0 = 2.f * quad_sum(add0); add1 = 2.f * quad_sum(add1);
         const float whole = F.whole;
+        float b0 = fmaf(add0, by0, whole * bound0), b1 = fmaf(add1, by1, whole * bound1);
+        if (__any_sync(0xffffffffu, fmaxf(b0, b1) > 32768.f || (b0 < 16.f && b0 > 0.f) || (b1 < 16.f && b1 > 0.f))) {
+            settle(add0 * by0, add1 * by1);
+            b0 = fmaf(add0, by0, whole * bound0); b1 = fmaf(add1, by1, whole * bound1);
+        }
+        bound0 = b0; bound1 = b1;
+        split_tile(x, by0, by1, hi, lo);
 #pragma unroll
-        for (int j = 0; j < DKP / 8; ++j) {
-            float add[4] = {};
-            uint32_t b[4];
-            load_matrices_transposed(b, keys + (row_at_t ^ (16 * j)));
-            mma_f16(add, lo[0], b[0], b[1]);
-            mma_f16(add, lo[1], b[2], b[3]);
-            if (LO) {
-                uint32_t bl[4];
-                load_matrices_transposed(bl, keys + (row_at_t ^ (16 * j)) + 2 * kRows);
-                mma_f16(add, hi[0], bl[0], bl[1]);
-                mma_f16(add, hi[1], bl[2], bl[3]);
+        for (int j = 0; j < DKP / 8; j += 4) {
+            float add[4][4] = {};
+            uint32_t b[4][4], l[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                load_matrices_transposed(b[i], keys + (row_at_t ^ (16 * (j + i))));
+                if (LO) load_matrices_transposed(l[i], keys + (row_at_t ^ (16 * (j + i))) + 2 * kRows);
             }
-            mma_f16(add, hi[0], b[0], b[1]);
-            mma_f16(add, hi[1], b[2], b[3]);
-            S[j][0] = fmaf(add[0], back0, whole * S[j][0]);
-            S[j][1] = fmaf(add[1], back0, whole * S[j][1]);
-            S[j][2] = fmaf(add[2], back1, whole * S[j][2]);
-            S[j][3] = fmaf(add[3], back1, whole * S[j][3]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(add[i], lo[0], b[i][0], b[i][1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(add[i], lo[1], b[i][2], b[i][3]);
+            if (LO) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mma_f16(add[i], hi[0], l[i][0], l[i][1]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mma_f16(add[i], hi[1], l[i][2], l[i][3]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(add[i], hi[0], b[i][0], b[i][1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(add[i], hi[1], b[i][2], b[i][3]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) S[j + i][k] = fmaf(whole, S[j + i][k], add[i][k]);
         }
     }
     copies_wait<0>();
@@ -584,7 +624,7 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = 8 * j + 2 * t + (i & 1), col = col0 + 2 * g + (i >> 1);
-            if (r < a.k_dim && col < a.v_dim) home[(long long)r * a.v_dim + col] = S[j][i];
+            if (r < a.k_dim && col < a.v_dim) home[(long long)r * a.v_dim + col] = S[j][i] * (i >> 1 ? back1 : back0);
         }
 }
 
@@ -606,22 +646,16 @@ int64_t delta_chunk_bytes(int64_t tokens, int64_t sequences, int k_heads, int v_
     return (tokens / kChunk + sequences) * ((int64_t)k_heads * key_bytes(k_dim, dtype) + (int64_t)v_heads * kHeadBytes);
 }
 
-template <typename T, int DKP>
+template <typename T, int DKP, int W>
 static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
     DeltaChunkArgs w{};
     w.records = a.tokens / kChunk + a.sequences;
     w.key_bytes = key_bytes(DKP, sizeof(T) == 4 ? CSB_F32 : CSB_F16);
     w.keys = static_cast<uint8_t*>(workspace);
     w.heads = w.keys + w.records * a.k_heads * (int64_t)w.key_bytes;
-    // warps of a CTA share a head's records: as many as leave no SM without a CTA
-    const int tiles = (a.v_dim + 15) / 16;
-    w.tiles_a_cta = std::min(tiles, 8);
-    while (w.tiles_a_cta > 2 && (int64_t)a.sequences * a.v_heads * ((tiles + w.tiles_a_cta - 1) / w.tiles_a_cta) < 148) w.tiles_a_cta = (w.tiles_a_cta + 1) / 2;
-    w.groups = (tiles + w.tiles_a_cta - 1) / w.tiles_a_cta;
+    w.groups = (a.v_dim + W * 16 - 1) / (W * 16);
     w.pairs = a.v_dim % 2 == 0 && a.ldo % 2 == 0 && reinterpret_cast<uintptr_t>(a.o) % (2 * sizeof(T)) == 0;
     w.values_async = a.v_dim * sizeof(T) % 16 == 0 && a.ldv * sizeof(T) % 16 == 0 && reinterpret_cast<uintptr_t>(a.v) % 16 == 0;
-    w.stage_bytes = w.key_bytes + kHeadBytes + kChunk * (w.tiles_a_cta * 16 * (int)sizeof(T) + 16);
-    w.stages = 3 * w.stage_bytes <= 227 * 1024 ? 3 : 2;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -631,17 +665,26 @@ static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
     cfg.dynamicSmemBytes = sizeof(PrepareSmem<DKP, sizeof(T) == 4>);
     CSB_CUDA((cudaFuncSetAttribute(csb_delta_prepare_kernel<T, DKP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
     CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_prepare_kernel<T, DKP>, a, w)));
-    cfg.gridDim = dim3((unsigned)((int64_t)a.sequences * a.v_heads * w.groups)); cfg.blockDim = dim3((unsigned)w.tiles_a_cta * 32);
-    cfg.dynamicSmemBytes = (size_t)w.stages * w.stage_bytes;
-    CSB_CUDA((cudaFuncSetAttribute(csb_delta_chunk_kernel<T, DKP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
-    CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_chunk_kernel<T, DKP>, a, w)));
+    cfg.gridDim = dim3((unsigned)((int64_t)a.sequences * a.v_heads * w.groups)); cfg.blockDim = dim3(W * 32);
+    cfg.dynamicSmemBytes = stage_count<T, DKP, W>() * stage_bytes<T, DKP, W>();
+    CSB_CUDA((cudaFuncSetAttribute(csb_delta_chunk_kernel<T, DKP, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
+    CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_chunk_kernel<T, DKP, W>, a, w)));
     return CSB_OK;
 }
 
+// Warps of a CTA share a head's records: as many as leave no SM without a CTA.
+template <typename T, int DKP>
+static int launch_chunks_by_width(const DeltaArgs& a, void* workspace, void* stream) {
+    const int64_t heads = (int64_t)a.sequences * a.v_heads;
+    if (a.v_dim > 64 && heads * ((a.v_dim + 127) / 128) >= 148) return launch_chunks<T, DKP, 8>(a, workspace, stream);
+    if (a.v_dim > 32 && heads * ((a.v_dim + 63) / 64) >= 148) return launch_chunks<T, DKP, 4>(a, workspace, stream);
+    return launch_chunks<T, DKP, 2>(a, workspace, stream);
+}
 template <typename T>
 static int launch_chunks_of(const DeltaArgs& a, void* workspace, void* stream) {
     const int dkp = padded(a.k_dim);
-    return dkp == 64 ? launch_chunks<T, 64>(a, workspace, stream) : dkp == 128 ? launch_chunks<T, 128>(a, workspace, stream) : launch_chunks<T, 256>(a, workspace, stream);
+    return dkp == 64 ? launch_chunks_by_width<T, 64>(a, workspace, stream) : dkp == 128 ? launch_chunks_by_width<T, 128>(a, workspace, stream)
+                                                                                       : launch_chunks_by_width<T, 256>(a, workspace, stream);
 }
 
 int launch_delta_chunks(int dtype, const DeltaArgs& a, void* workspace, void* stream) {
