@@ -19,6 +19,7 @@
 // bounded, and values that are not finite, which products with zeros would carry to tokens in front of them.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "csb_host.hpp"
 #include "csb_delta_slot.cuh"
@@ -298,67 +299,89 @@ __device__ __forceinline__ float settled(float largest, float back) {
     const float f = scale_of<8>(largest, inverse);
     return largest > 0.f ? fminf(f, 0x1p100f * back) : 1.f;
 }
+// The KS warps of a tile.
+template <int KS>
+__device__ __forceinline__ void tile_barrier(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(KS * 32) : "memory"); }
 // d += x M^T for a 32 x 32 matrix without an upper part; `at` is this lane's place in it, `lo` where its second half lies.
-// (The product of the two second halves is left out: 2^-22.)
+// (The product of the two second halves is left out: 2^-22.)  Tiles FROM .. TO - 1 of eight tokens are computed.
+template <int FROM, int TO>
 __device__ __forceinline__ void times_lower(float (&d)[4][4], const uint32_t (&hi)[2][4], const uint32_t (&lo)[2][4], uint32_t at, uint32_t lo_at) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {                               // (tiles in turn: a product waits for the one before it on its tile)
+        constexpr int kNone = 4;
+        const int from = FROM > 2 * s ? FROM : 2 * s < TO ? 2 * s : kNone;
         uint32_t b[2][4], l[2][4];
 #pragma unroll
-        for (int p = s; p < 2; ++p) { load_matrices(b[p], (at ^ (32 * s)) + p * 16 * 64); load_matrices(l[p], (at ^ (32 * s)) + p * 16 * 64 + lo_at); }
+        for (int p = from >> 1; 2 * p < TO; ++p) { load_matrices(b[p], (at ^ (32 * s)) + p * 16 * 64); load_matrices(l[p], (at ^ (32 * s)) + p * 16 * 64 + lo_at); }
 #pragma unroll
-        for (int i = 2 * s; i < 4; ++i) mma_f16(d[i], lo[s], b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+        for (int i = from; i < TO; ++i) mma_f16(d[i], lo[s], b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
 #pragma unroll
-        for (int i = 2 * s; i < 4; ++i) mma_f16(d[i], hi[s], l[i >> 1][(i & 1) * 2], l[i >> 1][(i & 1) * 2 + 1]);
+        for (int i = from; i < TO; ++i) mma_f16(d[i], hi[s], l[i >> 1][(i & 1) * 2], l[i >> 1][(i & 1) * 2 + 1]);
 #pragma unroll
-        for (int i = 2 * s; i < 4; ++i) mma_f16(d[i], hi[s], b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+        for (int i = from; i < TO; ++i) mma_f16(d[i], hi[s], b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
     }
 }
 
-// Tokens [first, first + n) one by one in fp32 on a warp's part of the state.
-template <typename T, int DKP>
-__device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)[DKP / 8][4], int h, int hk, int col0, long long first, int n) {
-    const int lane = threadIdx.x & 31, t = lane & 3;
+// Tokens [first, first + n) one by one in fp32, a warp's part of the state (keys' columns k0 .. k0 + 63).  `sums` is shared by
+// the tile's warps, which meet at barrier `id`.
+template <typename T, int KS>
+__device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)[8][4], int h, int hk, int col0, int part, long long first, int n, float* sums,
+                                                  int id) {
+    const int lane = threadIdx.x & 31, t = lane & 3, g = lane >> 2, k0 = part * 64;
     for (long long at = first; at < first + n; ++at) {
         const T *kp = static_cast<const T*>(a.k) + (long long)hk * a.k_dim + at * a.ldk, *qp = static_cast<const T*>(a.q) + (long long)hk * a.k_dim + at * a.ldq;
-        float kk = 0.f, qq = 0.f, dot = 0.f, u[2] = {0.f, 0.f}, o[2] = {0.f, 0.f};
+        float kk = 0.f, qq = 0.f, dot = 0.f, u[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int c = lane; c < a.k_dim; c += 32) {
+            const float x = to_float(kp[c]), y = to_float(qp[c]);
+            kk = fmaf(x, x, kk); qq = fmaf(y, y, qq); dot = fmaf(x, y, dot);
+        }
 #pragma unroll
-        for (int j = 0; j < DKP / 8; ++j) {
-            if (j % 4 == 0) asm volatile("" ::: "memory");       // (few loads in flight, few registers: the path is rare)
+        for (int d = 16; d; d >>= 1) {
+            kk += __shfl_xor_sync(0xffffffffu, kk, d); qq += __shfl_xor_sync(0xffffffffu, qq, d); dot += __shfl_xor_sync(0xffffffffu, dot, d);
+        }
+        float key[8][2];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int c = 8 * j + 2 * t + e;
-                if (c >= a.k_dim) continue;
-                const float x = to_float(kp[c]), y = to_float(qp[c]);
-                kk = fmaf(x, x, kk); qq = fmaf(y, y, qq); dot = fmaf(x, y, dot);
+                const int c = k0 + 8 * j + 2 * t + e;
+                const float x = c < a.k_dim ? to_float(kp[c]) : 0.f, y = c < a.k_dim ? to_float(qp[c]) : 0.f;
+                key[j][e] = x;
                 u[0] = fmaf(x, S[j][e], u[0]); u[1] = fmaf(x, S[j][2 + e], u[1]);
-                o[0] = fmaf(y, S[j][e], o[0]); o[1] = fmaf(y, S[j][2 + e], o[1]);
+                u[2] = fmaf(y, S[j][e], u[2]); u[3] = fmaf(y, S[j][2 + e], u[3]);
             }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = quad_sum(u[i]);
+        if (KS > 1) {
+            float4* s4 = reinterpret_cast<float4*>(sums);
+            if (t == 0) s4[part * 8 + g] = make_float4(u[0], u[1], u[2], u[3]);
+            tile_barrier<KS>(id);
+            u[0] = u[1] = u[2] = u[3] = 0.f;
+#pragma unroll
+            for (int p = 0; p < KS; ++p) {
+                const float4 f = s4[p * 8 + g];
+                u[0] += f.x; u[1] += f.y; u[2] += f.z; u[3] += f.w;
+            }
+            tile_barrier<KS>(id);
         }
-        kk = quad_sum(kk); qq = quad_sum(qq); dot = quad_sum(dot);
         const float kn = a.normalize ? 1.f / sqrtf(kk + kDeltaEps) : 1.f, qn = a.scale * (a.normalize ? 1.f / sqrtf(qq + kDeltaEps) : 1.f);
         const float decay = expf(a.g[at * a.ldg + h]), beta = a.beta[at * a.ldb + h];
         float add[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const int col = col0 + 2 * (lane >> 2) + r;
-            const float seen = decay * kn * quad_sum(u[r]), old = decay * quad_sum(o[r]);
+            const int col = col0 + 2 * g + r;
             const float v = col < a.v_dim ? to_float(static_cast<const T*>(a.v)[at * a.ldv + (long long)h * a.v_dim + col]) : 0.f;
-            add[r] = kn * (beta * (v - seen));
-            if (t == 0 && col < a.v_dim) static_cast<T*>(a.o)[at * a.ldo + (long long)h * a.v_dim + col] = from_float<T>(qn * (old + dot * add[r]));
+            add[r] = kn * (beta * (v - decay * kn * u[r]));
+            if (part == 0 && t == 0 && col < a.v_dim)
+                static_cast<T*>(a.o)[at * a.ldo + (long long)h * a.v_dim + col] = from_float<T>(qn * (decay * u[2 + r] + dot * add[r]));
         }
 #pragma unroll
-        for (int j = 0; j < DKP / 8; ++j) {
-            if (j % 4 == 0) asm volatile("" ::: "memory");
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int c = 8 * j + 2 * t + e;
-                if (c >= a.k_dim) continue;
-                const float x = to_float(kp[c]);
-                S[j][e] = fmaf(x, add[0], decay * S[j][e]);
-                S[j][2 + e] = fmaf(x, add[1], decay * S[j][2 + e]);
+                S[j][e] = fmaf(key[j][e], add[0], decay * S[j][e]);
+                S[j][2 + e] = fmaf(key[j][e], add[1], decay * S[j][2 + e]);
             }
-        }
     }
 }
 
@@ -369,22 +392,26 @@ __device__ __forceinline__ void store_pair(float* p, float x, float y) { *reinte
 __device__ __forceinline__ void store_pair(__half* p, float x, float y) { *reinterpret_cast<__half2*>(p) = __floats2half2_rn(x, y); }
 __device__ __forceinline__ void store_pair(__nv_bfloat16* p, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y); }
 
-// Shared memory of a chunk: the records and the values of W tiles.  Three chunks where they fit, else two.
-template <typename T, int DKP, int W>
-__host__ __device__ constexpr int stage_bytes() { return (sizeof(T) == 4 ? 4 : 2) * kChunk * DKP * 2 + kHeadBytes + kChunk * (W * 16 * (int)sizeof(T) + 16); }
-template <typename T, int DKP, int W>
-__host__ __device__ constexpr int stage_count() { return 3 * stage_bytes<T, DKP, W>() <= 227 * 1024 ? 3 : 2; }
+// A CTA has four warps: KS of them share a tile of 16 columns of the head, each with 64 of the keys' columns, and W = 4 / KS tiles
+// share the records.  Shared memory: two stages of a chunk's records and values, and what the warps of a tile tell one another.
+template <typename T, int KS>
+struct ChunkStage {
+    static constexpr int kTiles = 4 / KS, kKeyRows = kChunk * KS * 128, kKeyBytes = (sizeof(T) == 4 ? 4 : 2) * kKeyRows;
+    static constexpr int kValues = kTiles * 16, kPitch = kValues * (int)sizeof(T) + 16;
+    static constexpr int kBytes = kKeyBytes + kHeadBytes + (kChunk * kPitch + 511) / 512 * 512;
+    static constexpr int kTold = KS > 1 ? 4096 : 0;             // of a warp: [16 | 16][32 lanes] floats
+    static constexpr int kSmem = 2 * kBytes + 4 * kTold;
+};
 
-template <typename T, int DKP, int W>
-__global__ void __launch_bounds__(W * 32, 1) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
+template <typename T, int KS>
+__global__ void __launch_bounds__(128, 3) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
     constexpr bool LO = sizeof(T) == 4;
-    constexpr int kRows = kChunk * DKP * 2;
-    constexpr int kKeyBytes = (LO ? 4 : 2) * kRows;
-    constexpr int kStage = stage_bytes<T, DKP, W>(), kStages = stage_count<T, DKP, W>();
+    using Stage = ChunkStage<T, KS>;
+    constexpr int kRows = Stage::kKeyRows, kPitch = Stage::kPitch;
     extern __shared__ __align__(512) uint8_t smem[];
     pdl_launch_dependents();
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, tile = warp / KS, part = warp % KS;
     const int group = (int)(blockIdx.x % w.groups);
     const long long rest = blockIdx.x / w.groups;
     const int h = (int)(rest % a.v_heads), seq = (int)(rest / a.v_heads), hk = h / (a.v_heads / a.k_heads);
@@ -395,17 +422,17 @@ __global__ void __launch_bounds__(W * 32, 1) csb_delta_chunk_kernel(const DeltaA
         if (slot < 0) return;
     }
     if (t0 >= t1) return;
-    // Rows g and g + 8 of a tile, which a lane has, are neighbouring columns of the head.  (A warp behind the last column works on zeros.)
-    const int col0 = (group * W + warp) * 16;
-    float S[DKP / 8][4];
+    // Rows g and g + 8 of a tile, which a lane has, are neighbouring columns of the head.  (A tile behind the last column works on zeros.)
+    const int first_col = group * Stage::kValues, col0 = first_col + tile * 16, col = col0 + 2 * g;
+    float S[8][4];
     float* home = a.state + ((slot < 0 ? 0 : slot) * a.v_heads + h) * (long long)a.k_dim * a.v_dim;
     const bool from_zero = slot < 0 || (a.fresh && a.fresh[seq]);
 #pragma unroll
-    for (int j = 0; j < DKP / 8; ++j)
+    for (int j = 0; j < 8; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = 8 * j + 2 * t + (i & 1), col = col0 + 2 * g + (i >> 1);
-            S[j][i] = !from_zero && r < a.k_dim && col < a.v_dim ? home[(long long)r * a.v_dim + col] : 0.f;
+            const int r = part * 64 + 8 * j + 2 * t + (i & 1);
+            S[j][i] = !from_zero && r < a.k_dim && col + (i >> 1) < a.v_dim ? home[(long long)r * a.v_dim + col + (i >> 1)] : 0.f;
         }
     // The state is held times a power of two a row (by, its inverse back), such that it fits binary16 with room to
     // grow: its bound (kept up to date by what every chunk adds at most) stays within 2^4 .. 2^15, and where it leaves that, the
@@ -414,14 +441,14 @@ __global__ void __launch_bounds__(W * 32, 1) csb_delta_chunk_kernel(const DeltaA
     auto settle = [&](float add0, float add1) {
         float m0 = 0.f, m1 = 0.f;
 #pragma unroll
-        for (int j = 0; j < DKP / 8; ++j) {
+        for (int j = 0; j < 8; ++j) {
             m0 = fmaxf(m0, fmaxf(fabsf(S[j][0]), fabsf(S[j][1])));
             m1 = fmaxf(m1, fmaxf(fabsf(S[j][2]), fabsf(S[j][3])));
         }
         m0 = quad_max(m0); m1 = quad_max(m1);
         const float f0 = settled(fmaxf(m0, add0), back0), f1 = settled(fmaxf(m1, add1), back1);
 #pragma unroll
-        for (int j = 0; j < DKP / 8; ++j) { S[j][0] *= f0; S[j][1] *= f0; S[j][2] *= f1; S[j][3] *= f1; }
+        for (int j = 0; j < 8; ++j) { S[j][0] *= f0; S[j][1] *= f0; S[j][2] *= f1; S[j][3] *= f1; }
         by0 *= f0; by1 *= f1; back0 /= f0; back1 /= f1;
         bound0 = m0 * f0; bound1 = m1 * f1;
     };
@@ -429,61 +456,57 @@ __global__ void __launch_bounds__(W * 32, 1) csb_delta_chunk_kernel(const DeltaA
 
     const int tokens = (int)(t1 - t0), chunks = (tokens + kChunk - 1) / kChunk;
     const long long rec0 = t0 / kChunk + seq;
-    // Chunk c's records and its values of the CTA's columns (zeros where there are none), the next free stage.
-    const int first_col = group * W * 16;
-    constexpr int kValues = W * 16, kPitch = kValues * (int)sizeof(T) + 16;
     const T* vp = static_cast<const T*>(a.v) + t0 * a.ldv + (long long)h * a.v_dim + first_col;
     const uint8_t *keys_at = w.keys + (rec0 * a.k_heads + hk) * w.key_bytes + threadIdx.x * 16;
     const uint8_t *head_at = w.heads + (rec0 * a.v_heads + h) * kHeadBytes + threadIdx.x * 16;
     const long long keys_step = (long long)a.k_heads * w.key_bytes, head_step = (long long)a.v_heads * kHeadBytes;
-    constexpr int kUnit = 16 / (int)sizeof(T), kUnits = kValues / kUnit;      // values of 16 bytes, and such of a row
-    constexpr int kHeadUsed = kFactors + (int)sizeof(DeltaFactors);
-    int put_stage = 0;
+    // Chunk c's records and its values of the CTA's columns (zeros where there are none).
     auto fetch = [&](int c) {
         if (c < chunks) {
-            const uint32_t to = smem_u32(smem) + put_stage * kStage + threadIdx.x * 16;
+            uint8_t* stage = smem + (c & 1) * Stage::kBytes;
+            const uint32_t to = smem_u32(stage) + threadIdx.x * 16;
+            constexpr int kStep = 128 * 16, kUsed = kFactors + (int)sizeof(DeltaFactors);
 #pragma unroll
-            for (int i = 0; i < kKeyBytes; i += W * 512) copy_16(to + i, keys_at + i, 16);
+            for (int i = 0; i < Stage::kKeyBytes; i += kStep) copy_16(to + i, keys_at + i, 16);
 #pragma unroll
-            for (int i = 0; i < kHeadUsed; i += W * 512)
-                if (i + W * 512 <= kHeadUsed || i + (int)threadIdx.x * 16 < kHeadUsed) copy_16(to + kKeyBytes + i, head_at + i, 16);
+            for (int i = 0; i < kUsed; i += kStep)
+                if (i + kStep <= kUsed || i + (int)threadIdx.x * 16 < kUsed) copy_16(to + Stage::kKeyBytes + i, head_at + i, 16);
             keys_at += keys_step; head_at += head_step;
+            constexpr int kUnit = 16 / (int)sizeof(T), kUnits = Stage::kValues / kUnit;      // values of 16 bytes, and such of a row
+            uint8_t* values = stage + Stage::kKeyBytes + kHeadBytes;
             if (w.values_async) {
 #pragma unroll
-                for (int i = 0; i < kChunk * kUnits; i += W * 32) {
+                for (int i = 0; i < kChunk * kUnits; i += 128) {
                     const int row = (i + (int)threadIdx.x) / kUnits, u = (i + (int)threadIdx.x) % kUnits * kUnit, at = c * kChunk + row;
+                    if (kChunk * kUnits % 128 && row >= kChunk) break;
                     const bool there = at < tokens && first_col + u < a.v_dim;
-                    copy_16(smem_u32(smem) + put_stage * kStage + kKeyBytes + kHeadBytes + row * kPitch + u * (int)sizeof(T), there ? vp + at * a.ldv + u : vp, there ? 16 : 0);
+                    copy_16(smem_u32(values) + row * kPitch + u * (int)sizeof(T), there ? vp + at * a.ldv + u : vp, there ? 16 : 0);
                 }
             } else {
-                T* out = reinterpret_cast<T*>(smem + put_stage * kStage + kKeyBytes + kHeadBytes);
-                for (int i = threadIdx.x; i < kChunk * kValues; i += W * 32) {
-                    const int at = c * kChunk + i / kValues, u = i % kValues;
-                    out[(i / kValues) * (kPitch / (int)sizeof(T)) + u] = at < tokens && first_col + u < a.v_dim ? vp[at * a.ldv + u] : from_float<T>(0.f);
+                for (int i = threadIdx.x; i < kChunk * Stage::kValues; i += 128) {
+                    const int row = i / Stage::kValues, u = i % Stage::kValues, at = c * kChunk + row;
+                    reinterpret_cast<T*>(values + row * kPitch)[u] = at < tokens && first_col + u < a.v_dim ? vp[at * a.ldv + u] : from_float<T>(0.f);
                 }
             }
         }
         copies_commit();
-        if (++put_stage == kStages) put_stage = 0;
     };
-    const int col = col0 + 2 * g;                               // this lane's first column
+    fetch(0);
     const bool pairs = w.pairs && col + 1 < a.v_dim;
     T* op = static_cast<T*>(a.o) + t0 * a.ldo + (long long)h * a.v_dim + col;
-    fetch(0);
-    if (kStages == 3) fetch(1);
+    float* told = reinterpret_cast<float*>(smem + 2 * Stage::kBytes + tile * KS * Stage::kTold);
     // this lane's places in the operands (see load_matrices): rows are tokens, units 32 bytes a step apart
     const int tok = (lane >> 4) * 8 + (lane & 7);
-    const uint32_t row_at = tok * DKP * 2 + (((lane >> 3 & 1) ^ (tok & 7)) << 4), row_at_t = lane * DKP * 2 + ((lane & 7) << 4);
+    const uint32_t row_at = tok * KS * 128 + (((lane >> 3 & 1) ^ (tok & 7)) << 4), row_at_t = lane * KS * 128 + ((lane & 7) << 4);
     const uint32_t mat_at = matrix_at(tok, (lane >> 3 & 1) * 8);
-    for (int c = 0, stage = 0; c < chunks; ++c) {
-        copies_wait<kStages - 2>();
+    for (int c = 0; c < chunks; ++c) {
+        copies_wait<0>();
         __syncthreads();                                        // chunk c is there, and everybody is done with chunk c - 1
-        fetch(c + kStages - 1);
-        const uint8_t* here = smem + stage * kStage;
-        const uint32_t keys = smem_u32(here), head = keys + kKeyBytes;
-        const DeltaFactors& F = *reinterpret_cast<const DeltaFactors*>(here + kKeyBytes + kFactors);
-        const uint8_t* mine = here + kKeyBytes + kHeadBytes + (warp * 16 + 2 * g) * (int)sizeof(T) + 2 * t * kPitch;
-        if (++stage == kStages) stage = 0;
+        fetch(c + 1);
+        const uint8_t* here = smem + (c & 1) * Stage::kBytes;
+        const uint32_t keys = smem_u32(here) + part * 128, head = smem_u32(here) + Stage::kKeyBytes;
+        const DeltaFactors& F = *reinterpret_cast<const DeltaFactors*>(here + Stage::kKeyBytes + kFactors);
+        const uint8_t* mine = here + Stage::kKeyBytes + kHeadBytes + (tile * 16 + 2 * g) * (int)sizeof(T) + 2 * t * kPitch;
         float v[4][4], zero = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -491,86 +514,122 @@ __global__ void __launch_bounds__(W * 32, 1) csb_delta_chunk_kernel(const DeltaA
             v[i >> 1][i & 1] = f.x; v[i >> 1][2 + (i & 1)] = f.y;
             zero = fmaf(f.x, 0.f, fmaf(f.y, 0.f, zero));
         }
-        if (__any_sync(0xffffffffu, F.irregular || zero != 0.f)) {
+        if (__any_sync(0xffffffffu, F.irregular || zero != 0.f)) {     // (the warps of a tile agree)
 #pragma unroll
-            for (int j = 0; j < DKP / 8; ++j) { S[j][0] *= back0; S[j][1] *= back0; S[j][2] *= back1; S[j][3] *= back1; }
+            for (int j = 0; j < 8; ++j) { S[j][0] *= back0; S[j][1] *= back0; S[j][2] *= back1; S[j][3] *= back1; }
             by0 = by1 = back0 = back1 = 1.f;
-            walk_chunk_tokens<T, DKP>(a, S, h, hk, col0, t0 + (long long)c * kChunk, min(kChunk, tokens - c * kChunk));
+            walk_chunk_tokens<T, KS>(a, S, h, hk, col0, part, t0 + (long long)c * kChunk, min(kChunk, tokens - c * kChunk), told, 1 + tile);
             settle(0.f, 0.f);
             continue;
         }
         // S^T k and S^T q
         float r[4][4] = {}, o[4][4] = {};
 #pragma unroll
-        for (int j = 0; j < DKP / 16; ++j) {
+        for (int j = 0; j < 4; ++j) {
             uint32_t hi[4], lo[4], b[2][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float* p = &S[2 * j + (i >> 1)][(i & 1) * 2];
-                split_pair(p[0], p[1], hi[i], lo[i]);
-            }
+            for (int i = 0; i < 4; ++i) split_pair(S[2 * j + (i >> 1)][(i & 1) * 2], S[2 * j + (i >> 1)][(i & 1) * 2 + 1], hi[i], lo[i]);
             const uint32_t at = keys + (row_at ^ (32 * j));
             load_matrices(b[0], at);
             load_matrices(b[1], at + kRows / 2);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mma_f16(r[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
-#pragma unroll
             for (int i = 0; i < 4; ++i) mma_f16(r[i], lo, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
-            load_matrices(b[0], at + kRows);
-            load_matrices(b[1], at + kRows + kRows / 2);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mma_f16(o[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mma_f16(o[i], lo, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+            for (int i = 0; i < 4; ++i) mma_f16(r[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
             if (LO) {
                 load_matrices(b[0], at + 2 * kRows);
                 load_matrices(b[1], at + 2 * kRows + kRows / 2);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mma_f16(r[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+            }
+            load_matrices(b[0], at + kRows);
+            load_matrices(b[1], at + kRows + kRows / 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(o[i], lo, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(o[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+            if (LO) {
                 load_matrices(b[0], at + 3 * kRows);
                 load_matrices(b[1], at + 3 * kRows + kRows / 2);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mma_f16(o[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
             }
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            r[i][0] *= back0; r[i][1] *= back0; r[i][2] *= back1; r[i][3] *= back1;
+            o[i][0] *= back0; o[i][1] *= back0; o[i][2] *= back1; o[i][3] *= back1;
+        }
+        if (KS > 1) {
+            // the parts' sums, in the same order for all
+            float4* out = reinterpret_cast<float4*>(told) + part * 256 + lane;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                out[i * 32] = make_float4(r[i][0], r[i][1], r[i][2], r[i][3]);
+                out[(4 + i) * 32] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+            }
+            tile_barrier<KS>(1 + tile);
+            const float4* in = reinterpret_cast<const float4*>(told) + lane;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float4 f = in[i * 32];
+#pragma unroll
+                for (int p = 1; p < KS; ++p) { const float4 e = in[p * 256 + i * 32]; f.x += e.x; f.y += e.y; f.z += e.z; f.w += e.w; }
+                r[i][0] = f.x; r[i][1] = f.y; r[i][2] = f.z; r[i][3] = f.w;
+            }
+        }
         // what the tokens bring, less what the state holds for their keys
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float2 put = *reinterpret_cast<const float2*>(&F.put[8 * i + 2 * t]), keep = *reinterpret_cast<const float2*>(&F.keep[8 * i + 2 * t]);
-            const float2 fs = *reinterpret_cast<const float2*>(&F.from_state[8 * i + 2 * t]);
-            v[i][0] = fmaf(-keep.x, r[i][0] * back0, put.x * v[i][0]);
-            v[i][1] = fmaf(-keep.y, r[i][1] * back0, put.y * v[i][1]);
-            v[i][2] = fmaf(-keep.x, r[i][2] * back1, put.x * v[i][2]);
-            v[i][3] = fmaf(-keep.y, r[i][3] * back1, put.y * v[i][3]);
-            o[i][0] *= fs.x * back0; o[i][1] *= fs.y * back0; o[i][2] *= fs.x * back1; o[i][3] *= fs.y * back1;
+            v[i][0] = fmaf(-keep.x, r[i][0], put.x * v[i][0]);
+            v[i][1] = fmaf(-keep.y, r[i][1], put.y * v[i][1]);
+            v[i][2] = fmaf(-keep.x, r[i][2], put.x * v[i][2]);
+            v[i][3] = fmaf(-keep.y, r[i][3], put.y * v[i][3]);
         }
         uint32_t hi[2][4], lo[2][4];
         float x[4][4] = {}, inv0, inv1;
         split_rows(v, hi, lo, inv0, inv1);
-        times_lower(x, hi, lo, head + kSolveHi + mat_at, kSolveLo - kSolveHi);
+        times_lower<0, 4>(x, hi, lo, head + kSolveHi + mat_at, kSolveLo - kSolveHi);
 #pragma unroll
         for (int i = 0; i < 4; ++i) { x[i][0] *= inv0; x[i][1] *= inv0; x[i][2] *= inv1; x[i][3] *= inv1; }
-        // the chunk's own part of the outputs
+        // the outputs of the part's tokens (a tile's warps share them evenly)
         split_rows(x, hi, lo, inv0, inv1);
-        float inner[4][4] = {};
-        times_lower(inner, hi, lo, head + kInnerHi + mat_at, kInnerLo - kInnerHi);
+        constexpr int kMine = 4 / KS;
+        auto outputs = [&](auto from) {
+            constexpr int FROM = decltype(from)::value;
+            float inner[4][4] = {};
+            times_lower<FROM, FROM + kMine>(inner, hi, lo, head + kInnerHi + mat_at, kInnerLo - kInnerHi);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 fc = *reinterpret_cast<const float2*>(&F.from_chunk[8 * i + 2 * t]);
+            for (int i = FROM; i < FROM + kMine; ++i) {
+                float4 f = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+                if (KS > 1) {
+                    const float4* in = reinterpret_cast<const float4*>(told) + (4 + i) * 32 + lane;
+                    f = in[0];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float f = k ? fc.y : fc.x, x0 = fmaf(inner[i][k], f * inv0, o[i][k]), x1 = fmaf(inner[i][2 + k], f * inv1, o[i][2 + k]);
-                const int at = c * kChunk + 8 * i + 2 * t + k;
-                T* p = op + at * a.ldo;
-                if (at < tokens) {
-                    if (pairs) store_pair(p, x0, x1);
-                    else if (col < a.v_dim) {
-                        p[0] = from_float<T>(x0);
-                        if (col + 1 < a.v_dim) p[1] = from_float<T>(x1);
+                    for (int p = 1; p < KS; ++p) { const float4 e = in[p * 256]; f.x += e.x; f.y += e.y; f.z += e.z; f.w += e.w; }
+                }
+                const float2 fs = *reinterpret_cast<const float2*>(&F.from_state[8 * i + 2 * t]), fc = *reinterpret_cast<const float2*>(&F.from_chunk[8 * i + 2 * t]);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float ci = k ? fc.y : fc.x, cs = k ? fs.y : fs.x;
+                    const float x0 = fmaf(inner[i][k], ci * inv0, cs * (k ? f.y : f.x)), x1 = fmaf(inner[i][2 + k], ci * inv1, cs * (k ? f.w : f.z));
+                    const int at = c * kChunk + 8 * i + 2 * t + k;
+                    T* p = op + at * a.ldo;
+                    if (at < tokens) {
+                        if (pairs) store_pair(p, x0, x1);
+                        else if (col < a.v_dim) {
+                            p[0] = from_float<T>(x0);
+                            if (col + 1 < a.v_dim) p[1] = from_float<T>(x1);
+                        }
                     }
                 }
             }
-        }
+        };
+        if (KS == 1 || part == 0) outputs(std::integral_constant<int, 0>());
+        else if (KS == 2 || part == 2) outputs(std::integral_constant<int, 2>());
+        else if (part == 1) outputs(std::integral_constant<int, KS == 4 ? 1 : 0>());
+        else outputs(std::integral_constant<int, KS == 4 ? 3 : 0>());
         // the state behind the chunk (a scaled key's values are below 2)
         float add0 = 0.f, add1 = 0.f;
 #pragma unroll
@@ -589,7 +648,7 @@ __global__ void __launch_bounds__(W * 32, 1) csb_delta_chunk_kernel(const DeltaA
         bound0 = b0; bound1 = b1;
         split_tile(x, by0, by1, hi, lo);
 #pragma unroll
-        for (int j = 0; j < DKP / 8; j += 4) {
+        for (int j = 0; j < 8; j += 4) {
             float add[4][4] = {};
             uint32_t b[4][4], l[4][4];
 #pragma unroll
@@ -620,11 +679,11 @@ __global__ void __launch_bounds__(W * 32, 1) csb_delta_chunk_kernel(const DeltaA
     copies_wait<0>();
     if (slot < 0) return;
 #pragma unroll
-    for (int j = 0; j < DKP / 8; ++j)
+    for (int j = 0; j < 8; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = 8 * j + 2 * t + (i & 1), col = col0 + 2 * g + (i >> 1);
-            if (r < a.k_dim && col < a.v_dim) home[(long long)r * a.v_dim + col] = S[j][i] * (i >> 1 ? back1 : back0);
+            const int r = part * 64 + 8 * j + 2 * t + (i & 1);
+            if (r < a.k_dim && col + (i >> 1) < a.v_dim) home[(long long)r * a.v_dim + col + (i >> 1)] = S[j][i] * (i >> 1 ? back1 : back0);
         }
 }
 
@@ -646,14 +705,16 @@ int64_t delta_chunk_bytes(int64_t tokens, int64_t sequences, int k_heads, int v_
     return (tokens / kChunk + sequences) * ((int64_t)k_heads * key_bytes(k_dim, dtype) + (int64_t)v_heads * kHeadBytes);
 }
 
-template <typename T, int DKP, int W>
+template <typename T, int KS>
 static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
+    constexpr int DKP = KS * 64;
+    using Stage = ChunkStage<T, KS>;
     DeltaChunkArgs w{};
     w.records = a.tokens / kChunk + a.sequences;
-    w.key_bytes = key_bytes(DKP, sizeof(T) == 4 ? CSB_F32 : CSB_F16);
+    w.key_bytes = Stage::kKeyBytes;
     w.keys = static_cast<uint8_t*>(workspace);
     w.heads = w.keys + w.records * a.k_heads * (int64_t)w.key_bytes;
-    w.groups = (a.v_dim + W * 16 - 1) / (W * 16);
+    w.groups = (a.v_dim + Stage::kValues - 1) / Stage::kValues;
     w.pairs = a.v_dim % 2 == 0 && a.ldo % 2 == 0 && reinterpret_cast<uintptr_t>(a.o) % (2 * sizeof(T)) == 0;
     w.values_async = a.v_dim * sizeof(T) % 16 == 0 && a.ldv * sizeof(T) % 16 == 0 && reinterpret_cast<uintptr_t>(a.v) % 16 == 0;
     cudaLaunchAttribute attr[1];
@@ -665,26 +726,16 @@ static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
     cfg.dynamicSmemBytes = sizeof(PrepareSmem<DKP, sizeof(T) == 4>);
     CSB_CUDA((cudaFuncSetAttribute(csb_delta_prepare_kernel<T, DKP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
     CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_prepare_kernel<T, DKP>, a, w)));
-    cfg.gridDim = dim3((unsigned)((int64_t)a.sequences * a.v_heads * w.groups)); cfg.blockDim = dim3(W * 32);
-    cfg.dynamicSmemBytes = stage_count<T, DKP, W>() * stage_bytes<T, DKP, W>();
-    CSB_CUDA((cudaFuncSetAttribute(csb_delta_chunk_kernel<T, DKP, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
-    CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_chunk_kernel<T, DKP, W>, a, w)));
+    cfg.gridDim = dim3((unsigned)((int64_t)a.sequences * a.v_heads * w.groups)); cfg.blockDim = dim3(128);
+    cfg.dynamicSmemBytes = Stage::kSmem;
+    CSB_CUDA((cudaFuncSetAttribute(csb_delta_chunk_kernel<T, KS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
+    CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_chunk_kernel<T, KS>, a, w)));
     return CSB_OK;
-}
-
-// Warps of a CTA share a head's records: as many as leave no SM without a CTA.
-template <typename T, int DKP>
-static int launch_chunks_by_width(const DeltaArgs& a, void* workspace, void* stream) {
-    const int64_t heads = (int64_t)a.sequences * a.v_heads;
-    if (a.v_dim > 64 && heads * ((a.v_dim + 127) / 128) >= 148) return launch_chunks<T, DKP, 8>(a, workspace, stream);
-    if (a.v_dim > 32 && heads * ((a.v_dim + 63) / 64) >= 148) return launch_chunks<T, DKP, 4>(a, workspace, stream);
-    return launch_chunks<T, DKP, 2>(a, workspace, stream);
 }
 template <typename T>
 static int launch_chunks_of(const DeltaArgs& a, void* workspace, void* stream) {
     const int dkp = padded(a.k_dim);
-    return dkp == 64 ? launch_chunks_by_width<T, 64>(a, workspace, stream) : dkp == 128 ? launch_chunks_by_width<T, 128>(a, workspace, stream)
-                                                                                       : launch_chunks_by_width<T, 256>(a, workspace, stream);
+    return dkp == 64 ? launch_chunks<T, 1>(a, workspace, stream) : dkp == 128 ? launch_chunks<T, 2>(a, workspace, stream) : launch_chunks<T, 4>(a, workspace, stream);
 }
 
 int launch_delta_chunks(int dtype, const DeltaArgs& a, void* workspace, void* stream) {

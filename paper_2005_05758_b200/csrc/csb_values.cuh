@@ -74,8 +74,9 @@ __device__ __forceinline__ uint32_t half_pair(float x, float y) {
 }
 __device__ __forceinline__ void split_pair(float x, float y, uint32_t& hi, uint32_t& lo) {
     hi = half_pair(x, y);
-    const float2 f = pair_to_float(hi, __half());
-    lo = half_pair(x - f.x, y - f.y);
+    float dx, dy;                                         // hi - x in fp32, exact
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tsub.f32.f16 %0, l, %3;\n\tsub.f32.f16 %1, h, %4;\n\t}" : "=f"(dx), "=f"(dy) : "r"(hi), "f"(x), "f"(y));
+    lo = half_pair(-dx, -dy);
 }
 // D[16 x 8] += A[16 x 16] B[16 x 8] in binary16.  Lane 4g + t holds A at rows g, g + 8 (in turn) of columns 2t, 2t + 1 and
 // then 2t + 8, 2t + 9; B at the same rows of column g; D at (g, 2t), (g, 2t + 1), (g + 8, 2t), (g + 8, 2t + 1): two
