@@ -30,6 +30,7 @@ struct DeltaChunkArgs {
     long long records;
     int key_bytes, groups;              // of a key record; CTAs of a head
     int pairs, values_async;            // whether two neighbouring outputs are one access; whether v is copied 16 bytes at a time
+    int rows_aligned;                   // whether a lane's values of q and k are whole loads
 };
 
 // csb_delta_chunk.cu

@@ -69,16 +69,38 @@ __device__ __forceinline__ void sequence_range(const DeltaArgs& a, int i, long l
 constexpr int kPrepareWarps = 4;
 template <int DKP, bool LO>
 struct PrepareSmem {
-    uint8_t rows[LO ? 2 : 1][2][kChunk * DKP * 2];      // hi (and lo): keys, queries
+    union {
+        uint8_t rows[LO ? 2 : 1][2][kChunk * DKP * 2];  // hi (and lo): keys, queries
+        float lower[kPrepareWarps][kChunk][kChunk + 4]; // afterwards
+    };
     float dots[2 * kChunk][kChunk + 1];                 // of scaled rows: key . key, query . key
     float norm[2 * kChunk];                             // what a scaled row is to be multiplied by
-    float lower[kPrepareWarps][kChunk][kChunk + 4];
-    double sum[kPrepareWarps][kChunk];
     int odd;
 };
 
+// N values behind each other, 16 bytes a load at most.
+template <int N, typename T>
+__device__ __forceinline__ void load_run(const T* p, float (&x)[N]) {
+    if constexpr (N * sizeof(T) == 4) { const float2 f = pair_to_float(*reinterpret_cast<const uint32_t*>(p), T()); x[0] = f.x; x[1] = f.y; }
+    else if constexpr (N * sizeof(T) == 8 && sizeof(T) == 4) { const float2 f = *reinterpret_cast<const float2*>(p); x[0] = f.x; x[1] = f.y; }
+    else load_values(p, x);
+}
+// `lane` has a value of each of 16 rows: afterwards lanes 2i and 2i + 1 have the sum (or the largest) over all lanes of row i.
+template <typename F>
+__device__ __forceinline__ float reduce_rows(float (&x)[16], F&& join) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int n = 8, d = 16; n; n >>= 1, d >>= 1)
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float keep = lane & d ? x[i + n] : x[i], give = lane & d ? x[i] : x[i + n];
+            x[i] = join(keep, __shfl_xor_sync(0xffffffffu, give, d));
+        }
+    return join(x[0], __shfl_xor_sync(0xffffffffu, x[0], 1));
+}
+
 template <typename T, int DKP>
-__global__ void __launch_bounds__(kPrepareWarps * 32) csb_delta_prepare_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
+__global__ void __launch_bounds__(kPrepareWarps * 32, 5) csb_delta_prepare_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
     constexpr bool LO = sizeof(T) == 4;
     extern __shared__ __align__(512) uint8_t raw[];
     PrepareSmem<DKP, LO>& M = *reinterpret_cast<PrepareSmem<DKP, LO>*>(raw);
@@ -99,42 +121,52 @@ __global__ void __launch_bounds__(kPrepareWarps * 32) csb_delta_prepare_kernel(c
     if (threadIdx.x == 0) M.odd = 0;
     __syncthreads();
 
-    // rows 0 .. 31 are keys, 32 .. 63 queries; a warp takes 16 of them, a lane pairs of values 64 apart
-    constexpr int P = DKP / 64;
-    const T *kp = static_cast<const T*>(a.k) + (long long)hk * a.k_dim, *qp = static_cast<const T*>(a.q) + (long long)hk * a.k_dim;
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-        const int row = warp * 16 + i, t = row & (kChunk - 1);
-        const T* p = row < kChunk ? kp + (first + t) * a.ldk : qp + (first + t) * a.ldq;
-        float x[P][2], largest = 0.f, squares = 0.f;
-        bool finite = true;
+    // rows 0 .. 31 are keys, 32 .. 63 queries; a warp takes 16 of them, a lane N values of each
+    constexpr int N = DKP / 32;
+    const int col = lane * N, which = warp >> 1, each = a.v_heads / a.k_heads;
+    // (of the warp's first task below: loaded here so that it waits once)
+    const int h0 = hk * each + min(warp / 2, each - 1);
+    const float g0 = lane < n ? a.g[(first + lane) * a.ldg + h0] : 0.f, beta0 = lane < n ? a.beta[(first + lane) * a.ldb + h0] : 0.f;
+    {
+        const T* p0 = which ? static_cast<const T*>(a.q) + first * a.ldq : static_cast<const T*>(a.k) + first * a.ldk;
+        const long long ld = which ? a.ldq : a.ldk;
+        float x[16][N], m[16], s[16];
 #pragma unroll
-        for (int j = 0; j < P; ++j)
+        for (int i = 0; i < 16; ++i) {
+            const int t = (warp & 1) * 16 + i;
+            const T* p = p0 + t * ld + (long long)hk * a.k_dim + col;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int col = 64 * j + 2 * lane + e;
-                const float v = t < n && col < a.k_dim ? to_float(p[col]) : 0.f;
-                x[j][e] = v;
-                largest = fmaxf(largest, fabsf(v));
-                finite &= fabsf(v) <= kLargest;
-                squares = fmaf(v, v, squares);
+            for (int e = 0; e < N; ++e) x[i][e] = 0.f;
+            if (t < n) {
+                if (w.rows_aligned) { if (col < a.k_dim) load_run(p, x[i]); }
+                else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) if (col + e < a.k_dim) x[i][e] = to_float(p[e]);
+                }
             }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, d));
-            squares += __shfl_xor_sync(0xffffffffu, squares, d);
         }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            m[i] = s[i] = 0.f;
+#pragma unroll
+            for (int e = 0; e < N; ++e) { m[i] = fmaxf(m[i], fabsf(x[i][e])); s[i] = fmaf(x[i][e], x[i][e], s[i]); }
+        }
+        const float largest = reduce_rows(m, [](float p, float q) { return fmaxf(p, q); }), squares = reduce_rows(s, [](float p, float q) { return p + q; });
         float back;
         const float by = scale_of<0>(largest, back);
-        if (lane == 0) M.norm[row] = a.normalize ? back / sqrtf(squares + kDeltaEps) : back;
-        if (!finite || squares > kLargest) M.odd = 1;
+        if (!(squares <= kLargest)) M.odd = 1;                   // (a value that is not finite has no finite square)
+        if (!(lane & 1)) M.norm[warp * 16 + (lane >> 1)] = a.normalize ? back / sqrtf(squares + kDeltaEps) : back;
 #pragma unroll
-        for (int j = 0; j < P; ++j) {
-            const int at = operand_at<DKP>(t, 64 * j + 2 * lane), which = row >= kChunk;
-            uint32_t h, l;
-            split_pair(x[j][0] * by, x[j][1] * by, h, l);
-            *reinterpret_cast<uint32_t*>(&M.rows[0][which][at]) = h;
-            if (LO) *reinterpret_cast<uint32_t*>(&M.rows[LO ? 1 : 0][which][at]) = l;
+        for (int i = 0; i < 16; ++i) {
+            const float f = __shfl_sync(0xffffffffu, by, 2 * i);
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                const int at = operand_at<DKP>((warp & 1) * 16 + i, col + e);
+                uint32_t h, l;
+                split_pair(x[i][e] * f, x[i][e + 1] * f, h, l);
+                *reinterpret_cast<uint32_t*>(&M.rows[0][which][at]) = h;
+                if (LO) *reinterpret_cast<uint32_t*>(&M.rows[LO ? 1 : 0][which][at]) = l;
+            }
         }
     }
     __syncthreads();
@@ -146,7 +178,7 @@ __global__ void __launch_bounds__(kPrepareWarps * 32) csb_delta_prepare_kernel(c
     {
         // rows 16 warp .. + 15 of [keys; queries] times the keys
         float d[4][4] = {};
-        const int which = warp >> 1, row = (warp & 1) * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
+        const int row = (warp & 1) * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
         const uint32_t base_a = smem_u32(&M.rows[0][which][0]), base_b = smem_u32(&M.rows[0][0][0]);
         const uint32_t at_a = row * DKP * 2 + (((lane >> 4) ^ (row & 7)) << 4);
         const int tok = (lane >> 4) * 8 + (lane & 7);
@@ -178,50 +210,51 @@ __global__ void __launch_bounds__(kPrepareWarps * 32) csb_delta_prepare_kernel(c
     }
     __syncthreads();
 
-    // a warp a value head: lane s has column s of the matrices
-    const int each = a.v_heads / a.k_heads;
-    for (int e = warp; e < each; e += kPrepareWarps) {
-        const int h = hk * each + e;
+    // two tasks a value head, a warp each: the outputs' matrix, and the solved system with the factors.  Lane s has column s.
+    // Log-decays are summed from the column's token on (all of one sign: no difference of large sums, and -inf may be among them).
+    for (int task = warp; task < 2 * each; task += kPrepareWarps) {
+        const int h = hk * each + task / 2;
         uint8_t* out = w.heads + (rec * a.v_heads + h) * kHeadBytes;
         const bool there = lane < n;
-        const float g = there ? a.g[(first + lane) * a.ldg + h] : 0.f, beta = there ? a.beta[(first + lane) * a.ldb + h] : 0.f;
+        const float g = task == warp ? g0 : there ? a.g[(first + lane) * a.ldg + h] : 0.f;
+        float sum = 0.f;
+        if (task & 1) {
+#pragma unroll 8
+            for (int i = 0; i < kChunk; ++i) {
+                const float g_i = __shfl_sync(0xffffffffu, g, i);
+                sum = lane < i ? sum + g_i : 0.f;
+                const float p = lane <= i ? expf(sum) * M.dots[kChunk + i][lane] : 0.f;
+                const __half hi = __float2half_rn(p);
+                *reinterpret_cast<__half*>(out + kInnerHi + matrix_at(i, lane)) = hi;
+                *reinterpret_cast<__half*>(out + kInnerLo + matrix_at(i, lane)) = __float2half_rn(p - __half2float(hi));
+            }
+            continue;
+        }
+        const float beta = task == warp ? beta0 : there ? a.beta[(first + lane) * a.ldb + h] : 0.f;
+        const float norm = M.norm[lane], beta_norm = beta * norm;
         bool odd = M.odd || !(g <= 0.f) || !(fabsf(beta) <= kLargest);
-        // log-decays are summed in 64 bits, where the difference of two large sums is still a small one's; e^-10000 is 0 as e^-inf is
-        double G = g < -10000.f ? -10000.0 : (double)g;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const double before = __shfl_up_sync(0xffffffffu, G, d);
-            if (lane >= d) G += before;
-        }
-        M.sum[warp][lane] = G;
         float(&A)[kChunk][kChunk + 4] = M.lower[warp];
-        const float norm = M.norm[lane];
-        __syncwarp();
-#pragma unroll 4
+#pragma unroll 8
         for (int i = 0; i < kChunk; ++i) {
-            const float decay = lane <= i ? expf((float)(M.sum[warp][i] - G)) : 0.f;
-            const float beta_i = __shfl_sync(0xffffffffu, beta, i);
-            A[i][lane] = lane < i ? beta_i * M.norm[i] * norm * decay * M.dots[i][lane] : 0.f;
-            const float p = decay * M.dots[kChunk + i][lane];
-            const __half hi = __float2half_rn(p);
-            *reinterpret_cast<__half*>(out + kInnerHi + matrix_at(i, lane)) = hi;
-            *reinterpret_cast<__half*>(out + kInnerLo + matrix_at(i, lane)) = __float2half_rn(p - __half2float(hi));
+            const float g_i = __shfl_sync(0xffffffffu, g, i), f_i = __shfl_sync(0xffffffffu, beta_norm, i);
+            sum = lane < i ? sum + g_i : 0.f;
+            A[i][lane] = lane < i ? -f_i * norm * expf(sum) * M.dots[i][lane] : 0.f;
         }
         __syncwarp();
-        // column `lane` of the inverse of 1 + A, from the top down
+        // column `lane` of the inverse of 1 - A, from the top down
         float x[kChunk];
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) {
-            float s0 = lane == i ? 1.f : 0.f, s1 = 0.f;
+            float s[4] = {lane == i ? 1.f : 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int m = 0; m < i; m += 4) {
                 const float4 r = *reinterpret_cast<const float4*>(&A[i][m]);
-                s0 = fmaf(-r.x, x[m], s0);
-                if (m + 1 < i) s1 = fmaf(-r.y, x[m + 1], s1);
-                if (m + 2 < i) s0 = fmaf(-r.z, x[m + 2], s0);
-                if (m + 3 < i) s1 = fmaf(-r.w, x[m + 3], s1);
+                s[0] = fmaf(r.x, x[m], s[0]);
+                if (m + 1 < i) s[1] = fmaf(r.y, x[m + 1], s[1]);
+                if (m + 2 < i) s[2] = fmaf(r.z, x[m + 2], s[2]);
+                if (m + 3 < i) s[3] = fmaf(r.w, x[m + 3], s[3]);
             }
-            x[i] = s0 + s1;
+            x[i] = (s[0] + s[1]) + (s[2] + s[3]);
         }
         float largest = 0.f;
 #pragma unroll
@@ -240,15 +273,20 @@ __global__ void __launch_bounds__(kPrepareWarps * 32) csb_delta_prepare_kernel(c
             *reinterpret_cast<__half*>(out + kSolveLo + matrix_at(i, lane)) = __float2half_rn(v - __half2float(hi));
         }
         DeltaFactors& F = *reinterpret_cast<DeltaFactors*>(out + kFactors);
-        const double end = M.sum[warp][kChunk - 1];
-        const float from = expf((float)G), qn = a.scale * M.norm[kChunk + lane];
+        float G = g;                                             // from the chunk's first token
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const float before = __shfl_up_sync(0xffffffffu, G, d);
+            if (lane >= d) G += before;
+        }
+        const float from = expf(G), qn = a.scale * M.norm[kChunk + lane];
         F.put[lane] = back;
         F.keep[lane] = back * from * norm;
         F.from_state[lane] = from * qn;
         F.from_chunk[lane] = qn;
-        F.to_end[lane] = expf((float)(end - G));
+        F.to_end[lane] = expf(sum);
         odd = __any_sync(0xffffffffu, odd);
-        if (lane == 0) { F.whole = expf((float)end); F.irregular = odd; }
+        if (lane == 31) { F.whole = from; F.irregular = odd; }
         __syncwarp();
     }
 }
@@ -716,6 +754,9 @@ static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
     w.heads = w.keys + w.records * a.k_heads * (int64_t)w.key_bytes;
     w.groups = (a.v_dim + Stage::kValues - 1) / Stage::kValues;
     w.pairs = a.v_dim % 2 == 0 && a.ldo % 2 == 0 && reinterpret_cast<uintptr_t>(a.o) % (2 * sizeof(T)) == 0;
+    const size_t run = std::min<size_t>(DKP / 32 * sizeof(T), 16);
+    w.rows_aligned = a.k_dim % (DKP / 32) == 0 && a.k_dim * sizeof(T) % run == 0 && a.ldq * sizeof(T) % run == 0 && a.ldk * sizeof(T) % run == 0 &&
+                     reinterpret_cast<uintptr_t>(a.q) % run == 0 && reinterpret_cast<uintptr_t>(a.k) % run == 0;
     w.values_async = a.v_dim * sizeof(T) % 16 == 0 && a.ldv * sizeof(T) % 16 == 0 && reinterpret_cast<uintptr_t>(a.v) % 16 == 0;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
