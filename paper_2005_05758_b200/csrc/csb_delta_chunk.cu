@@ -28,8 +28,8 @@
 
 namespace csb {
 
-// A head's record: binary16 [kChunk][kChunk] four times, rows of 64 bytes whose 16-byte units are exchanged by matrix_at,
-// then factors.
+// A head's record: binary16 [source token][target token] four times, rows of 64 bytes whose 16-byte units are exchanged by
+// matrix_at, then factors.
 enum : int { kSolveHi = 0, kSolveLo = 2048, kInnerHi = 4096, kInnerLo = 6144, kFactors = 8192 };
 struct DeltaFactors {
     float put[kChunk];                  // the scale of the solve matrix's column: V enters as put V - keep S^T k
@@ -85,6 +85,13 @@ __device__ __forceinline__ void load_run(const T* p, float (&x)[N]) {
     else if constexpr (N * sizeof(T) == 8 && sizeof(T) == 4) { const float2 f = *reinterpret_cast<const float2*>(p); x[0] = f.x; x[1] = f.y; }
     else load_values(p, x);
 }
+// Eight values as two halves, `lo` bytes apart.
+__device__ __forceinline__ void store_eight(uint8_t* at, int lo, const float (&x)[8]) {
+    uint4 h, l;
+    split_pair(x[0], x[1], h.x, l.x); split_pair(x[2], x[3], h.y, l.y); split_pair(x[4], x[5], h.z, l.z); split_pair(x[6], x[7], h.w, l.w);
+    *reinterpret_cast<uint4*>(at) = h;
+    *reinterpret_cast<uint4*>(at + lo) = l;
+}
 // `lane` has a value of each of 16 rows: afterwards lanes 2i and 2i + 1 have the sum (or the largest) over all lanes of row i.
 template <typename F>
 __device__ __forceinline__ float reduce_rows(float (&x)[16], F&& join) {
@@ -100,7 +107,7 @@ __device__ __forceinline__ float reduce_rows(float (&x)[16], F&& join) {
 }
 
 template <typename T, int DKP>
-__global__ void __launch_bounds__(kPrepareWarps * 32, 5) csb_delta_prepare_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
+__global__ void __launch_bounds__(kPrepareWarps * 32, DKP == 256 ? 3 : 5) csb_delta_prepare_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
     constexpr bool LO = sizeof(T) == 4;
     extern __shared__ __align__(512) uint8_t raw[];
     PrepareSmem<DKP, LO>& M = *reinterpret_cast<PrepareSmem<DKP, LO>*>(raw);
@@ -131,20 +138,22 @@ __global__ void __launch_bounds__(kPrepareWarps * 32, 5) csb_delta_prepare_kerne
         const T* p0 = which ? static_cast<const T*>(a.q) + first * a.ldq : static_cast<const T*>(a.k) + first * a.ldk;
         const long long ld = which ? a.ldq : a.ldk;
         float x[16][N], m[16], s[16];
+        // (a token or column that is not there reads one that is and drops it: a branch around a load would wait for every one)
+        p0 += (long long)hk * a.k_dim;
+        if (w.rows_aligned) {
+            const T* p = p0 + (col < a.k_dim ? col : 0);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int t = (warp & 1) * 16 + i;
-            const T* p = p0 + t * ld + (long long)hk * a.k_dim + col;
+            for (int i = 0; i < 16; ++i) load_run(p + min((warp & 1) * 16 + i, n - 1) * ld, x[i]);
+        } else {
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[i][e] = 0.f;
-            if (t < n) {
-                if (w.rows_aligned) { if (col < a.k_dim) load_run(p, x[i]); }
-                else {
+            for (int i = 0; i < 16; ++i)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) if (col + e < a.k_dim) x[i][e] = to_float(p[e]);
-                }
-            }
+                for (int e = 0; e < N; ++e) x[i][e] = to_float(p0[min((warp & 1) * 16 + i, n - 1) * ld + min(col + e, a.k_dim - 1)]);
         }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[i][e] = (warp & 1) * 16 + i < n && col + e < a.k_dim ? x[i][e] : 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             m[i] = s[i] = 0.f;
@@ -218,15 +227,18 @@ __global__ void __launch_bounds__(kPrepareWarps * 32, 5) csb_delta_prepare_kerne
         const bool there = lane < n;
         const float g = task == warp ? g0 : there ? a.g[(first + lane) * a.ldg + h] : 0.f;
         float sum = 0.f;
+        const float g2 = g * 1.44269504f;                        // (of 2 instead of e)
         if (task & 1) {
-#pragma unroll 8
-            for (int i = 0; i < kChunk; ++i) {
-                const float g_i = __shfl_sync(0xffffffffu, g, i);
-                sum = lane < i ? sum + g_i : 0.f;
-                const float p = lane <= i ? expf(sum) * M.dots[kChunk + i][lane] : 0.f;
-                const __half hi = __float2half_rn(p);
-                *reinterpret_cast<__half*>(out + kInnerHi + matrix_at(i, lane)) = hi;
-                *reinterpret_cast<__half*>(out + kInnerLo + matrix_at(i, lane)) = __float2half_rn(p - __half2float(hi));
+#pragma unroll
+            for (int i0 = 0; i0 < kChunk; i0 += 8) {
+                float p[8];
+#pragma unroll
+                for (int i = i0; i < i0 + 8; ++i) {
+                    const float g_i = __shfl_sync(0xffffffffu, g2, i), dot = M.dots[kChunk + i][lane];
+                    sum = lane < i ? sum + g_i : 0.f;
+                    p[i - i0] = exp2f(sum) * (lane <= i ? dot : 0.f);
+                }
+                store_eight(out + kInnerHi + matrix_at(lane, i0), kInnerLo - kInnerHi, p);
             }
             continue;
         }
@@ -234,11 +246,11 @@ __global__ void __launch_bounds__(kPrepareWarps * 32, 5) csb_delta_prepare_kerne
         const float norm = M.norm[lane], beta_norm = beta * norm;
         bool odd = M.odd || !(g <= 0.f) || !(fabsf(beta) <= kLargest);
         float(&A)[kChunk][kChunk + 4] = M.lower[warp];
-#pragma unroll 8
+#pragma unroll
         for (int i = 0; i < kChunk; ++i) {
-            const float g_i = __shfl_sync(0xffffffffu, g, i), f_i = __shfl_sync(0xffffffffu, beta_norm, i);
+            const float g_i = __shfl_sync(0xffffffffu, g2, i), f_i = __shfl_sync(0xffffffffu, beta_norm, i), dot = M.dots[i][lane];
             sum = lane < i ? sum + g_i : 0.f;
-            A[i][lane] = lane < i ? -f_i * norm * expf(sum) * M.dots[i][lane] : 0.f;
+            A[i][lane] = -f_i * norm * (exp2f(sum) * (lane < i ? dot : 0.f));
         }
         __syncwarp();
         // column `lane` of the inverse of 1 - A, from the top down
@@ -266,25 +278,25 @@ __global__ void __launch_bounds__(kPrepareWarps * 32, 5) csb_delta_prepare_kerne
         float back;
         const float by = scale_of<8>(largest, back);
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) {
-            const float v = x[i] * by;
-            const __half hi = __float2half_rn(v);
-            *reinterpret_cast<__half*>(out + kSolveHi + matrix_at(i, lane)) = hi;
-            *reinterpret_cast<__half*>(out + kSolveLo + matrix_at(i, lane)) = __float2half_rn(v - __half2float(hi));
+        for (int i0 = 0; i0 < kChunk; i0 += 8) {
+            float p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = x[i0 + i] * by;
+            store_eight(out + kSolveHi + matrix_at(lane, i0), kSolveLo - kSolveHi, p);
         }
         DeltaFactors& F = *reinterpret_cast<DeltaFactors*>(out + kFactors);
-        float G = g;                                             // from the chunk's first token
+        float G = g2;                                            // from the chunk's first token
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const float before = __shfl_up_sync(0xffffffffu, G, d);
             if (lane >= d) G += before;
         }
-        const float from = expf(G), qn = a.scale * M.norm[kChunk + lane];
+        const float from = exp2f(G), qn = a.scale * M.norm[kChunk + lane];
         F.put[lane] = back;
         F.keep[lane] = back * from * norm;
         F.from_state[lane] = from * qn;
         F.from_chunk[lane] = qn;
-        F.to_end[lane] = expf(sum);
+        F.to_end[lane] = exp2f(sum);
         odd = __any_sync(0xffffffffu, odd);
         if (lane == 31) { F.whole = from; F.irregular = odd; }
         __syncwarp();
@@ -340,7 +352,7 @@ __device__ __forceinline__ float settled(float largest, float back) {
 // The KS warps of a tile.
 template <int KS>
 __device__ __forceinline__ void tile_barrier(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(KS * 32) : "memory"); }
-// d += x M^T for a 32 x 32 matrix without an upper part; `at` is this lane's place in it, `lo` where its second half lies.
+// d += x M for a 32 x 32 matrix [source][target] without targets in front of their sources; `at` is this lane's place in it, `lo` where its second half lies.
 // (The product of the two second halves is left out: 2^-22.)  Tiles FROM .. TO - 1 of eight tokens are computed.
 template <int FROM, int TO>
 __device__ __forceinline__ void times_lower(float (&d)[4][4], const uint32_t (&hi)[2][4], const uint32_t (&lo)[2][4], uint32_t at, uint32_t lo_at) {
@@ -350,7 +362,7 @@ __device__ __forceinline__ void times_lower(float (&d)[4][4], const uint32_t (&h
         const int from = FROM > 2 * s ? FROM : 2 * s < TO ? 2 * s : kNone;
         uint32_t b[2][4], l[2][4];
 #pragma unroll
-        for (int p = from >> 1; 2 * p < TO; ++p) { load_matrices(b[p], (at ^ (32 * s)) + p * 16 * 64); load_matrices(l[p], (at ^ (32 * s)) + p * 16 * 64 + lo_at); }
+        for (int p = from >> 1; 2 * p < TO; ++p) { load_matrices_transposed(b[p], (at ^ (32 * p)) + s * 16 * 64); load_matrices_transposed(l[p], (at ^ (32 * p)) + s * 16 * 64 + lo_at); }
 #pragma unroll
         for (int i = from; i < TO; ++i) mma_f16(d[i], lo[s], b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
 #pragma unroll
@@ -536,7 +548,7 @@ __global__ void __launch_bounds__(128, 3) csb_delta_chunk_kernel(const DeltaArgs
     // this lane's places in the operands (see load_matrices): rows are tokens, units 32 bytes a step apart
     const int tok = (lane >> 4) * 8 + (lane & 7);
     const uint32_t row_at = tok * KS * 128 + (((lane >> 3 & 1) ^ (tok & 7)) << 4), row_at_t = lane * KS * 128 + ((lane & 7) << 4);
-    const uint32_t mat_at = matrix_at(tok, (lane >> 3 & 1) * 8);
+    const uint32_t mat_at = matrix_at((lane >> 3 & 1) * 8 + (lane & 7), (lane >> 4) * 8);
     for (int c = 0; c < chunks; ++c) {
         copies_wait<0>();
         __syncthreads();                                        // chunk c is there, and everybody is done with chunk c - 1
