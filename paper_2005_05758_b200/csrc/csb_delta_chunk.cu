@@ -375,7 +375,7 @@ __device__ __forceinline__ void times_lower(float (&d)[4][4], const uint32_t (&h
 // Tokens [first, first + n) one by one in fp32, a warp's part of the state (keys' columns k0 .. k0 + 63).  `sums` is shared by
 // the tile's warps, which meet at barrier `id`.
 template <typename T, int KS>
-__device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)[8][4], int h, int hk, int col0, int part, long long first, int n, float* sums,
+__device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)[8][4], int h, int hk, int col0, int part, long long first, int n, float4* sums,
                                                   int id) {
     const int lane = threadIdx.x & 31, t = lane & 3, g = lane >> 2, k0 = part * 64;
     for (long long at = first; at < first + n; ++at) {
@@ -403,13 +403,12 @@ __device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[i] = quad_sum(u[i]);
         if (KS > 1) {
-            float4* s4 = reinterpret_cast<float4*>(sums);
-            if (t == 0) s4[part * 8 + g] = make_float4(u[0], u[1], u[2], u[3]);
+            if (t == 0) sums[part * 8 + g] = make_float4(u[0], u[1], u[2], u[3]);
             tile_barrier<KS>(id);
             u[0] = u[1] = u[2] = u[3] = 0.f;
 #pragma unroll
             for (int p = 0; p < KS; ++p) {
-                const float4 f = s4[p * 8 + g];
+                const float4 f = sums[p * 8 + g];
                 u[0] += f.x; u[1] += f.y; u[2] += f.z; u[3] += f.w;
             }
             tile_barrier<KS>(id);
@@ -442,26 +441,32 @@ __device__ __forceinline__ void store_pair(float* p, float x, float y) { *reinte
 __device__ __forceinline__ void store_pair(__half* p, float x, float y) { *reinterpret_cast<__half2*>(p) = __floats2half2_rn(x, y); }
 __device__ __forceinline__ void store_pair(__nv_bfloat16* p, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y); }
 
-// A CTA has four warps: KS of them share a tile of 16 columns of the head, each with 64 of the keys' columns, and W = 4 / KS tiles
-// share the records.  Shared memory: two stages of a chunk's records and values, and what the warps of a tile tell one another.
+// A CTA has eight warps.  Four carry the state: KS of them share a tile of 16 columns of the head, each with 64 of the keys'
+// columns, and W = 4 / KS tiles share the records.  The other four, a chunk behind, compute the outputs from the operands
+// that the first hand over (the state's halves and V'), and fetch what comes next: none of that is on the way from chunk to chunk.
+// Shared memory: stages of a chunk's records and values, and what warps tell one another.
 template <typename T, int KS>
 struct ChunkStage {
     static constexpr int kTiles = 4 / KS, kKeyRows = kChunk * KS * 128, kKeyBytes = (sizeof(T) == 4 ? 4 : 2) * kKeyRows;
     static constexpr int kValues = kTiles * 16, kPitch = kValues * (int)sizeof(T) + 16;
     static constexpr int kBytes = kKeyBytes + kHeadBytes + (kChunk * kPitch + 511) / 512 * 512;
-    static constexpr int kTold = KS > 1 ? 4096 : 0;             // of a warp: [16 | 16][32 lanes] floats
-    static constexpr int kSmem = 2 * kBytes + 4 * kTold;
+    static constexpr int kState = 4096, kScales = 256, kNew = 2048;   // of a warp: halves of the state, scales of its rows; of a tile: V'
+    static constexpr int kHand = 4 * (kState + kScales) + kTiles * kNew + 512;
+    static constexpr int kTold = KS > 1 ? 8 * 2048 : 0;         // a warp's sums over its keys' columns
+    static constexpr int kStages = 3 * kBytes + 2 * kHand + kTold <= 227 * 1024 ? 3 : 2;
+    static constexpr int kSmem = kStages * kBytes + 2 * kHand + kTold;
 };
 
 template <typename T, int KS>
-__global__ void __launch_bounds__(128, 3) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
+__global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
     constexpr bool LO = sizeof(T) == 4;
     using Stage = ChunkStage<T, KS>;
     constexpr int kRows = Stage::kKeyRows, kPitch = Stage::kPitch;
     extern __shared__ __align__(512) uint8_t smem[];
     pdl_launch_dependents();
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, tile = warp / KS, part = warp % KS;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, g = lane >> 2, t = lane & 3, tile = warp / KS, part = warp % KS;
+    const bool carries = threadIdx.x < 128;
     const int group = (int)(blockIdx.x % w.groups);
     const long long rest = blockIdx.x / w.groups;
     const int h = (int)(rest % a.v_heads), seq = (int)(rest / a.v_heads), hk = h / (a.v_heads / a.k_heads);
@@ -482,7 +487,7 @@ __global__ void __launch_bounds__(128, 3) csb_delta_chunk_kernel(const DeltaArgs
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = part * 64 + 8 * j + 2 * t + (i & 1);
-            S[j][i] = !from_zero && r < a.k_dim && col + (i >> 1) < a.v_dim ? home[(long long)r * a.v_dim + col + (i >> 1)] : 0.f;
+            S[j][i] = carries && !from_zero && r < a.k_dim && col + (i >> 1) < a.v_dim ? home[(long long)r * a.v_dim + col + (i >> 1)] : 0.f;
         }
     // The state is held times a power of two a row (by, its inverse back), such that it fits binary16 with room to
     // grow: its bound (kept up to date by what every chunk adds at most) stays within 2^4 .. 2^15, and where it leaves that, the
@@ -506,34 +511,36 @@ __global__ void __launch_bounds__(128, 3) csb_delta_chunk_kernel(const DeltaArgs
 
     const int tokens = (int)(t1 - t0), chunks = (tokens + kChunk - 1) / kChunk;
     const long long rec0 = t0 / kChunk + seq;
+    const int thread = threadIdx.x & 127;
     const T* vp = static_cast<const T*>(a.v) + t0 * a.ldv + (long long)h * a.v_dim + first_col;
-    const uint8_t *keys_at = w.keys + (rec0 * a.k_heads + hk) * w.key_bytes + threadIdx.x * 16;
-    const uint8_t *head_at = w.heads + (rec0 * a.v_heads + h) * kHeadBytes + threadIdx.x * 16;
+    const uint8_t *keys_at = w.keys + (rec0 * a.k_heads + hk) * w.key_bytes + thread * 16;
+    const uint8_t *head_at = w.heads + (rec0 * a.v_heads + h) * kHeadBytes + thread * 16;
     const long long keys_step = (long long)a.k_heads * w.key_bytes, head_step = (long long)a.v_heads * kHeadBytes;
     // Chunk c's records and its values of the CTA's columns (zeros where there are none).
+    auto stage_of = [&](int c) { return smem + (Stage::kStages == 3 ? c % 3 : c & 1) * Stage::kBytes; };
     auto fetch = [&](int c) {
         if (c < chunks) {
-            uint8_t* stage = smem + (c & 1) * Stage::kBytes;
-            const uint32_t to = smem_u32(stage) + threadIdx.x * 16;
+            uint8_t* stage = stage_of(c);
+            const uint32_t to = smem_u32(stage) + thread * 16;
             constexpr int kStep = 128 * 16, kUsed = kFactors + (int)sizeof(DeltaFactors);
 #pragma unroll
             for (int i = 0; i < Stage::kKeyBytes; i += kStep) copy_16(to + i, keys_at + i, 16);
 #pragma unroll
             for (int i = 0; i < kUsed; i += kStep)
-                if (i + kStep <= kUsed || i + (int)threadIdx.x * 16 < kUsed) copy_16(to + Stage::kKeyBytes + i, head_at + i, 16);
+                if (i + kStep <= kUsed || i + thread * 16 < kUsed) copy_16(to + Stage::kKeyBytes + i, head_at + i, 16);
             keys_at += keys_step; head_at += head_step;
             constexpr int kUnit = 16 / (int)sizeof(T), kUnits = Stage::kValues / kUnit;      // values of 16 bytes, and such of a row
             uint8_t* values = stage + Stage::kKeyBytes + kHeadBytes;
             if (w.values_async) {
 #pragma unroll
                 for (int i = 0; i < kChunk * kUnits; i += 128) {
-                    const int row = (i + (int)threadIdx.x) / kUnits, u = (i + (int)threadIdx.x) % kUnits * kUnit, at = c * kChunk + row;
+                    const int row = (i + thread) / kUnits, u = (i + thread) % kUnits * kUnit, at = c * kChunk + row;
                     if (kChunk * kUnits % 128 && row >= kChunk) break;
                     const bool there = at < tokens && first_col + u < a.v_dim;
                     copy_16(smem_u32(values) + row * kPitch + u * (int)sizeof(T), there ? vp + at * a.ldv + u : vp, there ? 16 : 0);
                 }
             } else {
-                for (int i = threadIdx.x; i < kChunk * Stage::kValues; i += 128) {
+                for (int i = thread; i < kChunk * Stage::kValues; i += 128) {
                     const int row = i / Stage::kValues, u = i % Stage::kValues, at = c * kChunk + row;
                     reinterpret_cast<T*>(values + row * kPitch)[u] = at < tokens && first_col + u < a.v_dim ? vp[at * a.ldv + u] : from_float<T>(0.f);
                 }
@@ -541,22 +548,31 @@ __global__ void __launch_bounds__(128, 3) csb_delta_chunk_kernel(const DeltaArgs
         }
         copies_commit();
     };
-    fetch(0);
     const bool pairs = w.pairs && col + 1 < a.v_dim;
     T* op = static_cast<T*>(a.o) + t0 * a.ldo + (long long)h * a.v_dim + col;
-    float* told = reinterpret_cast<float*>(smem + 2 * Stage::kBytes + tile * KS * Stage::kTold);
+    // what the carrying warps hand over, by turns; what the warps of a tile tell one another
+    uint8_t* hands = smem + Stage::kStages * Stage::kBytes;
+    float4* told = reinterpret_cast<float4*>(hands + 2 * Stage::kHand + ((carries ? 0 : 4) + tile * KS) * 2048);
+    const int meet = (carries ? 1 : 5) + tile;
+    struct Hand { uint4* state; float2* scales; float4* fresh; int* walked; };
+    auto hand_of = [&](int c) {
+        uint8_t* p = hands + (c & 1) * Stage::kHand;
+        return Hand{reinterpret_cast<uint4*>(p + warp * Stage::kState) + lane, reinterpret_cast<float2*>(p + 4 * Stage::kState + warp * Stage::kScales) + lane,
+                    reinterpret_cast<float4*>(p + 4 * (Stage::kState + Stage::kScales) + tile * Stage::kNew) + lane,
+                    reinterpret_cast<int*>(p + 4 * (Stage::kState + Stage::kScales) + Stage::kTiles * Stage::kNew) + tile};
+    };
     // this lane's places in the operands (see load_matrices): rows are tokens, units 32 bytes a step apart
     const int tok = (lane >> 4) * 8 + (lane & 7);
     const uint32_t row_at = tok * KS * 128 + (((lane >> 3 & 1) ^ (tok & 7)) << 4), row_at_t = lane * KS * 128 + ((lane & 7) << 4);
     const uint32_t mat_at = matrix_at((lane >> 3 & 1) * 8 + (lane & 7), (lane >> 4) * 8);
-    for (int c = 0; c < chunks; ++c) {
-        copies_wait<0>();
-        __syncthreads();                                        // chunk c is there, and everybody is done with chunk c - 1
-        fetch(c + 1);
-        const uint8_t* here = smem + (c & 1) * Stage::kBytes;
+
+    // From the state in front of chunk c to the one behind it.
+    auto carry = [&](int c) {
+        const uint8_t* here = stage_of(c);
         const uint32_t keys = smem_u32(here) + part * 128, head = smem_u32(here) + Stage::kKeyBytes;
         const DeltaFactors& F = *reinterpret_cast<const DeltaFactors*>(here + Stage::kKeyBytes + kFactors);
         const uint8_t* mine = here + Stage::kKeyBytes + kHeadBytes + (tile * 16 + 2 * g) * (int)sizeof(T) + 2 * t * kPitch;
+        const Hand out = hand_of(c);
         float v[4][4], zero = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -564,21 +580,26 @@ __global__ void __launch_bounds__(128, 3) csb_delta_chunk_kernel(const DeltaArgs
             v[i >> 1][i & 1] = f.x; v[i >> 1][2 + (i & 1)] = f.y;
             zero = fmaf(f.x, 0.f, fmaf(f.y, 0.f, zero));
         }
-        if (__any_sync(0xffffffffu, F.irregular || zero != 0.f)) {     // (the warps of a tile agree)
+        const bool walk = __any_sync(0xffffffffu, F.irregular || zero != 0.f);      // (the warps of a tile agree)
+        if (part == 0 && lane == 0) *out.walked = walk;
+        if (walk) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) { S[j][0] *= back0; S[j][1] *= back0; S[j][2] *= back1; S[j][3] *= back1; }
             by0 = by1 = back0 = back1 = 1.f;
-            walk_chunk_tokens<T, KS>(a, S, h, hk, col0, part, t0 + (long long)c * kChunk, min(kChunk, tokens - c * kChunk), told, 1 + tile);
+            walk_chunk_tokens<T, KS>(a, S, h, hk, col0, part, t0 + (long long)c * kChunk, min(kChunk, tokens - c * kChunk), told, meet);
             settle(0.f, 0.f);
-            continue;
+            return;
         }
-        // S^T k and S^T q
-        float r[4][4] = {}, o[4][4] = {};
+        // S^T k
+        float r[4][4] = {};
+        *out.scales = make_float2(back0, back1);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             uint32_t hi[4], lo[4], b[2][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) split_pair(S[2 * j + (i >> 1)][(i & 1) * 2], S[2 * j + (i >> 1)][(i & 1) * 2 + 1], hi[i], lo[i]);
+            out.state[2 * j * 32] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            out.state[(2 * j + 1) * 32] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
             const uint32_t at = keys + (row_at ^ (32 * j));
             load_matrices(b[0], at);
             load_matrices(b[1], at + kRows / 2);
@@ -592,39 +613,19 @@ __global__ void __launch_bounds__(128, 3) csb_delta_chunk_kernel(const DeltaArgs
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mma_f16(r[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
             }
-            load_matrices(b[0], at + kRows);
-            load_matrices(b[1], at + kRows + kRows / 2);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mma_f16(o[i], lo, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mma_f16(o[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
-            if (LO) {
-                load_matrices(b[0], at + 3 * kRows);
-                load_matrices(b[1], at + 3 * kRows + kRows / 2);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mma_f16(o[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
-            }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            r[i][0] *= back0; r[i][1] *= back0; r[i][2] *= back1; r[i][3] *= back1;
-            o[i][0] *= back0; o[i][1] *= back0; o[i][2] *= back1; o[i][3] *= back1;
-        }
+        for (int i = 0; i < 4; ++i) { r[i][0] *= back0; r[i][1] *= back0; r[i][2] *= back1; r[i][3] *= back1; }
         if (KS > 1) {
             // the parts' sums, in the same order for all
-            float4* out = reinterpret_cast<float4*>(told) + part * 256 + lane;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) told[part * 128 + i * 32 + lane] = make_float4(r[i][0], r[i][1], r[i][2], r[i][3]);
+            tile_barrier<KS>(meet);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                out[i * 32] = make_float4(r[i][0], r[i][1], r[i][2], r[i][3]);
-                out[(4 + i) * 32] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
-            }
-            tile_barrier<KS>(1 + tile);
-            const float4* in = reinterpret_cast<const float4*>(told) + lane;
+                float4 f = told[i * 32 + lane];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float4 f = in[i * 32];
-#pragma unroll
-                for (int p = 1; p < KS; ++p) { const float4 e = in[p * 256 + i * 32]; f.x += e.x; f.y += e.y; f.z += e.z; f.w += e.w; }
+                for (int p = 1; p < KS; ++p) { const float4 e = told[p * 128 + i * 32 + lane]; f.x += e.x; f.y += e.y; f.z += e.z; f.w += e.w; }
                 r[i][0] = f.x; r[i][1] = f.y; r[i][2] = f.z; r[i][3] = f.w;
             }
         }
@@ -643,43 +644,10 @@ __global__ void __launch_bounds__(128, 3) csb_delta_chunk_kernel(const DeltaArgs
         times_lower<0, 4>(x, hi, lo, head + kSolveHi + mat_at, kSolveLo - kSolveHi);
 #pragma unroll
         for (int i = 0; i < 4; ++i) { x[i][0] *= inv0; x[i][1] *= inv0; x[i][2] *= inv1; x[i][3] *= inv1; }
-        // the outputs of the part's tokens (a tile's warps share them evenly)
-        split_rows(x, hi, lo, inv0, inv1);
-        constexpr int kMine = 4 / KS;
-        auto outputs = [&](auto from) {
-            constexpr int FROM = decltype(from)::value;
-            float inner[4][4] = {};
-            times_lower<FROM, FROM + kMine>(inner, hi, lo, head + kInnerHi + mat_at, kInnerLo - kInnerHi);
+        if (part == 0) {
 #pragma unroll
-            for (int i = FROM; i < FROM + kMine; ++i) {
-                float4 f = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
-                if (KS > 1) {
-                    const float4* in = reinterpret_cast<const float4*>(told) + (4 + i) * 32 + lane;
-                    f = in[0];
-#pragma unroll
-                    for (int p = 1; p < KS; ++p) { const float4 e = in[p * 256]; f.x += e.x; f.y += e.y; f.z += e.z; f.w += e.w; }
-                }
-                const float2 fs = *reinterpret_cast<const float2*>(&F.from_state[8 * i + 2 * t]), fc = *reinterpret_cast<const float2*>(&F.from_chunk[8 * i + 2 * t]);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const float ci = k ? fc.y : fc.x, cs = k ? fs.y : fs.x;
-                    const float x0 = fmaf(inner[i][k], ci * inv0, cs * (k ? f.y : f.x)), x1 = fmaf(inner[i][2 + k], ci * inv1, cs * (k ? f.w : f.z));
-                    const int at = c * kChunk + 8 * i + 2 * t + k;
-                    T* p = op + at * a.ldo;
-                    if (at < tokens) {
-                        if (pairs) store_pair(p, x0, x1);
-                        else if (col < a.v_dim) {
-                            p[0] = from_float<T>(x0);
-                            if (col + 1 < a.v_dim) p[1] = from_float<T>(x1);
-                        }
-                    }
-                }
-            }
-        };
-        if (KS == 1 || part == 0) outputs(std::integral_constant<int, 0>());
-        else if (KS == 2 || part == 2) outputs(std::integral_constant<int, 2>());
-        else if (part == 1) outputs(std::integral_constant<int, KS == 4 ? 1 : 0>());
-        else outputs(std::integral_constant<int, KS == 4 ? 3 : 0>());
+            for (int i = 0; i < 4; ++i) out.fresh[i * 32] = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+        }
         // the state behind the chunk (a scaled key's values are below 2)
         float add0 = 0.f, add1 = 0.f;
 #pragma unroll
@@ -725,9 +693,103 @@ __global__ void __launch_bounds__(128, 3) csb_delta_chunk_kernel(const DeltaArgs
 #pragma unroll
                 for (int k = 0; k < 4; ++k) S[j + i][k] = fmaf(whole, S[j + i][k], add[i][k]);
         }
+    };
+
+    // The outputs of chunk c; the warps of a tile share its tokens evenly.
+    auto put_out = [&](int c) {
+        const uint8_t* here = stage_of(c);
+        const uint32_t queries = smem_u32(here) + kRows + part * 128, head = smem_u32(here) + Stage::kKeyBytes;
+        const DeltaFactors& F = *reinterpret_cast<const DeltaFactors*>(here + Stage::kKeyBytes + kFactors);
+        const Hand in = hand_of(c);
+        if (*in.walked) return;
+        float o[4][4] = {};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t b[2][4];
+            const uint4 h4 = in.state[2 * j * 32], l4 = in.state[(2 * j + 1) * 32];
+            const uint32_t hi[4] = {h4.x, h4.y, h4.z, h4.w}, lo[4] = {l4.x, l4.y, l4.z, l4.w};
+            const uint32_t at = queries + (row_at ^ (32 * j));
+            load_matrices(b[0], at);
+            load_matrices(b[1], at + kRows / 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(o[i], lo, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma_f16(o[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+            if (LO) {
+                load_matrices(b[0], at + 2 * kRows);
+                load_matrices(b[1], at + 2 * kRows + kRows / 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mma_f16(o[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+            }
+        }
+        const float2 back = *in.scales;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { o[i][0] *= back.x; o[i][1] *= back.x; o[i][2] *= back.y; o[i][3] *= back.y; }
+        if (KS > 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) told[part * 128 + i * 32 + lane] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+            tile_barrier<KS>(meet);
+        }
+        float x[4][4], inv0, inv1;
+        uint32_t hi[2][4], lo[2][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 f = in.fresh[i * 32];
+            x[i][0] = f.x; x[i][1] = f.y; x[i][2] = f.z; x[i][3] = f.w;
+        }
+        split_rows(x, hi, lo, inv0, inv1);
+        constexpr int kMine = 4 / KS;
+        auto outputs = [&](auto from) {
+            constexpr int FROM = decltype(from)::value;
+            float inner[4][4] = {};
+            times_lower<FROM, FROM + kMine>(inner, hi, lo, head + kInnerHi + mat_at, kInnerLo - kInnerHi);
+#pragma unroll
+            for (int i = FROM; i < FROM + kMine; ++i) {
+                float4 f = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+                if (KS > 1) {
+                    f = told[i * 32 + lane];
+#pragma unroll
+                    for (int p = 1; p < KS; ++p) { const float4 e = told[p * 128 + i * 32 + lane]; f.x += e.x; f.y += e.y; f.z += e.z; f.w += e.w; }
+                }
+                const float2 fs = *reinterpret_cast<const float2*>(&F.from_state[8 * i + 2 * t]), fc = *reinterpret_cast<const float2*>(&F.from_chunk[8 * i + 2 * t]);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float ci = k ? fc.y : fc.x, cs = k ? fs.y : fs.x;
+                    const float x0 = fmaf(inner[i][k], ci * inv0, cs * (k ? f.y : f.x)), x1 = fmaf(inner[i][2 + k], ci * inv1, cs * (k ? f.w : f.z));
+                    const int at = c * kChunk + 8 * i + 2 * t + k;
+                    T* p = op + at * a.ldo;
+                    if (at < tokens) {
+                        if (pairs) store_pair(p, x0, x1);
+                        else if (col < a.v_dim) {
+                            p[0] = from_float<T>(x0);
+                            if (col + 1 < a.v_dim) p[1] = from_float<T>(x1);
+                        }
+                    }
+                }
+            }
+        };
+        if (KS == 1 || part == 0) outputs(std::integral_constant<int, 0>());
+        else if (KS == 2 || part == 2) outputs(std::integral_constant<int, 2>());
+        else if (part == 1) outputs(std::integral_constant<int, KS == 4 ? 1 : 0>());
+        else outputs(std::integral_constant<int, KS == 4 ? 3 : 0>());
+    };
+
+    if (!carries) fetch(0);
+    for (int c = 0; c <= chunks; ++c) {
+        if (!carries) copies_wait<0>();
+        __syncthreads();                                        // chunk c is there, and what is handed over of chunk c - 1
+        if (carries) {
+            if (c < chunks) carry(c);
+        } else {
+            if (Stage::kStages == 3) fetch(c + 1);
+            if (c > 0) put_out(c - 1);
+        }
+        if (Stage::kStages == 2) {
+            __syncthreads();                                    // chunk c - 1 is done with
+            if (!carries) fetch(c + 1);
+        }
     }
-    copies_wait<0>();
-    if (slot < 0) return;
+    if (slot < 0 || !carries) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -779,7 +841,7 @@ static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
     cfg.dynamicSmemBytes = sizeof(PrepareSmem<DKP, sizeof(T) == 4>);
     CSB_CUDA((cudaFuncSetAttribute(csb_delta_prepare_kernel<T, DKP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
     CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_prepare_kernel<T, DKP>, a, w)));
-    cfg.gridDim = dim3((unsigned)((int64_t)a.sequences * a.v_heads * w.groups)); cfg.blockDim = dim3(128);
+    cfg.gridDim = dim3((unsigned)((int64_t)a.sequences * a.v_heads * w.groups)); cfg.blockDim = dim3(256);
     cfg.dynamicSmemBytes = Stage::kSmem;
     CSB_CUDA((cudaFuncSetAttribute(csb_delta_chunk_kernel<T, KS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
     CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_chunk_kernel<T, KS>, a, w)));
