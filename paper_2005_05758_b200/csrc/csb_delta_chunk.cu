@@ -39,7 +39,7 @@ struct DeltaFactors {
     float to_end[kChunk];               // e^(G_end - G_t)
     float whole;                        // e^(G_end)
     int irregular;
-    int pad[2];
+    float put_most, keep_most;          // largest put; largest keep times the sum of the key's magnitudes
 };
 constexpr int kHeadBytes = (kFactors + (int)sizeof(DeltaFactors) + 511) / 512 * 512;
 constexpr float kLargest = 3.402823466e38f;
@@ -75,6 +75,7 @@ struct PrepareSmem {
     };
     float dots[2 * kChunk][kChunk + 1];                 // of scaled rows: key . key, query . key
     float norm[2 * kChunk];                             // what a scaled row is to be multiplied by
+    float reach[2 * kChunk];                            // at least the sum of a scaled row's magnitudes
     int odd;
 };
 
@@ -164,6 +165,7 @@ __global__ void __launch_bounds__(kPrepareWarps * 32, DKP == 256 ? 3 : 5) csb_de
         float back;
         const float by = scale_of<0>(largest, back);
         if (!(squares <= kLargest)) M.odd = 1;                   // (a value that is not finite has no finite square)
+        if (!(lane & 1)) M.reach[warp * 16 + (lane >> 1)] = 1.001f * by * sqrtf((float)DKP * squares);
         if (!(lane & 1)) M.norm[warp * 16 + (lane >> 1)] = a.normalize ? back / sqrtf(squares + kDeltaEps) : back;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -297,8 +299,15 @@ __global__ void __launch_bounds__(kPrepareWarps * 32, DKP == 256 ? 3 : 5) csb_de
         F.from_state[lane] = from * qn;
         F.from_chunk[lane] = qn;
         F.to_end[lane] = exp2f(sum);
+        float put_most = back, keep_most = back * from * fabsf(norm) * M.reach[lane];
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            put_most = fmaxf(put_most, __shfl_xor_sync(0xffffffffu, put_most, d));
+            keep_most = fmaxf(keep_most, __shfl_xor_sync(0xffffffffu, keep_most, d));
+        }
+        odd |= !(keep_most <= kLargest);
         odd = __any_sync(0xffffffffu, odd);
-        if (lane == 31) { F.whole = from; F.irregular = odd; }
+        if (lane == 31) { F.whole = from; F.irregular = odd; F.put_most = put_most; F.keep_most = keep_most; }
         __syncwarp();
     }
 }
@@ -332,22 +341,13 @@ __device__ __forceinline__ void split_tile(const float (&x)[4][4], float by0, fl
             split_pair(p[0] * by, p[1] * by, hi[s][i], lo[s][i]);
         }
 }
-// The same, each row's largest value taken to 2^13; the inverse scales of rows g and g + 8.
-__device__ __forceinline__ void split_rows(const float (&x)[4][4], uint32_t (&hi)[2][4], uint32_t (&lo)[2][4], float& inv0, float& inv1) {
-    float m0 = 0.f, m1 = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        m0 = fmaxf(m0, fmaxf(fabsf(x[i][0]), fabsf(x[i][1])));
-        m1 = fmaxf(m1, fmaxf(fabsf(x[i][2]), fabsf(x[i][3])));
-    }
-    const float by0 = scale_of<13>(quad_max(m0), inv0), by1 = scale_of<13>(quad_max(m1), inv1);
-    split_tile(x, by0, by1, hi, lo);
-}
-// What takes a largest value into [2^8, 2^9), for a row that is divided by `back` to get its true values' scale (which stays below 2^100).
-__device__ __forceinline__ float settled(float largest, float back) {
+__device__ __forceinline__ float inverse_of(float power_of_two) { return __uint_as_float(0x7f000000u - __float_as_uint(power_of_two)); }
+// What takes a row's largest magnitude into [2^TOP, 2^(TOP + 1)) where it may be times 2^100 of its true size at most (`back`: from
+// its present size to its true one).
+template <int TOP>
+__device__ __forceinline__ float grow(float largest, float back) {
     float inverse;
-    const float f = scale_of<8>(largest, inverse);
-    return largest > 0.f ? fminf(f, 0x1p100f * back) : 1.f;
+    return fminf(scale_of<TOP>(largest, inverse), 0x1p100f * back);
 }
 // The KS warps of a tile.
 template <int KS>
@@ -441,24 +441,48 @@ __device__ __forceinline__ void store_pair(float* p, float x, float y) { *reinte
 __device__ __forceinline__ void store_pair(__half* p, float x, float y) { *reinterpret_cast<__half2*>(p) = __floats2half2_rn(x, y); }
 __device__ __forceinline__ void store_pair(__nv_bfloat16* p, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y); }
 
-// A CTA has eight warps.  Four carry the state: KS of them share a tile of 16 columns of the head, each with 64 of the keys'
-// columns, and W = 4 / KS tiles share the records.  The other four, a chunk behind, compute the outputs from the operands
-// that the first hand over (the state's halves and V'), and fetch what comes next: none of that is on the way from chunk to chunk.
+// A CTA has nine warps.  Four carry the state: KS of them share a tile of 16 columns of the head, each with 64 of the keys'
+// columns, and W = 4 / KS tiles share the records.  Four others, a chunk behind, compute the outputs from the operands
+// that the first hand over (the state's halves and V'), and the last fetches what comes next: none of that is on the way from
+// chunk to chunk.
 // Shared memory: stages of a chunk's records and values, and what warps tell one another.
 template <typename T, int KS>
 struct ChunkStage {
     static constexpr int kTiles = 4 / KS, kKeyRows = kChunk * KS * 128, kKeyBytes = (sizeof(T) == 4 ? 4 : 2) * kKeyRows;
     static constexpr int kValues = kTiles * 16, kPitch = kValues * (int)sizeof(T) + 16;
     static constexpr int kBytes = kKeyBytes + kHeadBytes + (kChunk * kPitch + 511) / 512 * 512;
-    static constexpr int kState = 4096, kScales = 256, kNew = 2048;   // of a warp: halves of the state, scales of its rows; of a tile: V'
+    static constexpr int kState = 4096, kScales = 512, kNew = 2048;   // of a warp: halves of the state, scales of its rows and of V'; of a tile: V'
     static constexpr int kHand = 4 * (kState + kScales) + kTiles * kNew + 512;
-    static constexpr int kTold = KS > 1 ? 8 * 2048 : 0;         // a warp's sums over its keys' columns
+    static constexpr int kTold = KS > 1 ? 8 * 2048 + 512 : 0;   // a warp's sums over its keys' columns; its rows' largest magnitudes
     static constexpr int kStages = 3 * kBytes + 2 * kHand + kTold <= 227 * 1024 ? 3 : 2;
     static constexpr int kSmem = kStages * kBytes + 2 * kHand + kTold;
 };
 
+// The sequence with the rank-th most tokens, so that long ones start first (12 sequences of 1 to 1300 tokens on 16 heads: the call 187 us
+// instead of 213).
+// Where there are more sequences than that is worth, the rank-th as they come.  All threads of the block take part.
+constexpr int kRanked = 256;
+__device__ __forceinline__ int sequence_of_rank(const DeltaArgs& a, int rank) {
+    __shared__ int length[kRanked], found;
+    if (!a.seq_begin || a.sequences > kRanked) return rank;
+    const int i = threadIdx.x;
+    if (i < a.sequences) {
+        long long t0, t1;
+        sequence_range(a, i, t0, t1);
+        length[i] = (int)(t1 - t0);
+    }
+    __syncthreads();
+    if (i < a.sequences) {
+        int before = 0;
+        for (int j = 0; j < a.sequences; ++j) before += length[j] > length[i] || (length[j] == length[i] && j < i);
+        if (before == rank) found = i;
+    }
+    __syncthreads();
+    return found;
+}
+
 template <typename T, int KS>
-__global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
+__global__ void __launch_bounds__(288, 1) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
     constexpr bool LO = sizeof(T) == 4;
     using Stage = ChunkStage<T, KS>;
     constexpr int kRows = Stage::kKeyRows, kPitch = Stage::kPitch;
@@ -466,10 +490,10 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, g = lane >> 2, t = lane & 3, tile = warp / KS, part = warp % KS;
-    const bool carries = threadIdx.x < 128;
+    const bool carries = threadIdx.x < 128, fetches = threadIdx.x >= 256;
     const int group = (int)(blockIdx.x % w.groups);
     const long long rest = blockIdx.x / w.groups;
-    const int h = (int)(rest % a.v_heads), seq = (int)(rest / a.v_heads), hk = h / (a.v_heads / a.k_heads);
+    const int h = (int)(rest % a.v_heads), seq = sequence_of_rank(a, (int)(rest / a.v_heads)), hk = h / (a.v_heads / a.k_heads);
     long long t0, t1, slot = -1;
     sequence_range(a, seq, t0, t1);
     if (a.state) {
@@ -489,58 +513,60 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
             const int r = part * 64 + 8 * j + 2 * t + (i & 1);
             S[j][i] = carries && !from_zero && r < a.k_dim && col + (i >> 1) < a.v_dim ? home[(long long)r * a.v_dim + col + (i >> 1)] : 0.f;
         }
-    // The state is held times a power of two a row (by, its inverse back), such that it fits binary16 with room to
-    // grow: its bound (kept up to date by what every chunk adds at most) stays within 2^4 .. 2^15, and where it leaves that, the
-    // row's largest value is looked up and taken to 2^8.  What a chunk adds, `add` at most in all, is scaled alike.
-    float by0 = 1.f, by1 = 1.f, back0 = 1.f, back1 = 1.f, bound0, bound1;
-    auto settle = [&](float add0, float add1) {
-        float m0 = 0.f, m1 = 0.f;
+    // The state is held times a power of two a row (by, its inverse back) that binary16 halves of it can have.  No scale waits for
+    // the values it is for: with the row's largest magnitude (most) of the state in front of the chunk and of the chunk's v, bounds
+    // on S^T k, V' and the state behind the chunk follow from what the record says, and each is scaled by its bound.  A bound is
+    // at most about 2^14 above the values; a half's step is 2^-24 at values up to 2^14, so 22 bits of the values stay.
+    float by0 = 1.f, by1 = 1.f, back0 = 1.f, back1 = 1.f, most0, most1;
+    auto largest = [&]() {
+        most0 = most1 = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            m0 = fmaxf(m0, fmaxf(fabsf(S[j][0]), fabsf(S[j][1])));
-            m1 = fmaxf(m1, fmaxf(fabsf(S[j][2]), fabsf(S[j][3])));
+            most0 = fmaxf(most0, fmaxf(fabsf(S[j][0]), fabsf(S[j][1])));
+            most1 = fmaxf(most1, fmaxf(fabsf(S[j][2]), fabsf(S[j][3])));
         }
-        m0 = quad_max(m0); m1 = quad_max(m1);
-        const float f0 = settled(fmaxf(m0, add0), back0), f1 = settled(fmaxf(m1, add1), back1);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) { S[j][0] *= f0; S[j][1] *= f0; S[j][2] *= f1; S[j][3] *= f1; }
-        by0 *= f0; by1 *= f1; back0 /= f0; back1 /= f1;
-        bound0 = m0 * f0; bound1 = m1 * f1;
+        most0 = quad_max(most0); most1 = quad_max(most1);
     };
-    settle(0.f, 0.f);
+    auto settle = [&]() {                                        // from true values
+        largest();
+        by0 = grow<8>(most0, 1.f); by1 = grow<8>(most1, 1.f);
+        back0 = inverse_of(by0); back1 = inverse_of(by1);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { S[j][0] *= by0; S[j][1] *= by0; S[j][2] *= by1; S[j][3] *= by1; }
+        most0 *= by0; most1 *= by1;
+    };
+    settle();
 
     const int tokens = (int)(t1 - t0), chunks = (tokens + kChunk - 1) / kChunk;
     const long long rec0 = t0 / kChunk + seq;
-    const int thread = threadIdx.x & 127;
     const T* vp = static_cast<const T*>(a.v) + t0 * a.ldv + (long long)h * a.v_dim + first_col;
-    const uint8_t *keys_at = w.keys + (rec0 * a.k_heads + hk) * w.key_bytes + thread * 16;
-    const uint8_t *head_at = w.heads + (rec0 * a.v_heads + h) * kHeadBytes + thread * 16;
+    const uint8_t *keys_at = w.keys + (rec0 * a.k_heads + hk) * w.key_bytes + lane * 16;
+    const uint8_t *head_at = w.heads + (rec0 * a.v_heads + h) * kHeadBytes + lane * 16;
     const long long keys_step = (long long)a.k_heads * w.key_bytes, head_step = (long long)a.v_heads * kHeadBytes;
     // Chunk c's records and its values of the CTA's columns (zeros where there are none).
     auto stage_of = [&](int c) { return smem + (Stage::kStages == 3 ? c % 3 : c & 1) * Stage::kBytes; };
     auto fetch = [&](int c) {
         if (c < chunks) {
             uint8_t* stage = stage_of(c);
-            const uint32_t to = smem_u32(stage) + thread * 16;
-            constexpr int kStep = 128 * 16, kUsed = kFactors + (int)sizeof(DeltaFactors);
-#pragma unroll
-            for (int i = 0; i < Stage::kKeyBytes; i += kStep) copy_16(to + i, keys_at + i, 16);
-#pragma unroll
-            for (int i = 0; i < kUsed; i += kStep)
-                if (i + kStep <= kUsed || i + thread * 16 < kUsed) copy_16(to + Stage::kKeyBytes + i, head_at + i, 16);
+            const uint32_t to = smem_u32(stage) + lane * 16;
+            constexpr int kUsed = kFactors + (int)sizeof(DeltaFactors);
+#pragma unroll 8
+            for (int i = 0; i < Stage::kKeyBytes; i += 512) copy_16(to + i, keys_at + i, 16);
+#pragma unroll 8
+            for (int i = 0; i < kUsed; i += 512)
+                if (i + lane * 16 < kUsed) copy_16(to + Stage::kKeyBytes + i, head_at + i, 16);
             keys_at += keys_step; head_at += head_step;
             constexpr int kUnit = 16 / (int)sizeof(T), kUnits = Stage::kValues / kUnit;      // values of 16 bytes, and such of a row
             uint8_t* values = stage + Stage::kKeyBytes + kHeadBytes;
             if (w.values_async) {
-#pragma unroll
-                for (int i = 0; i < kChunk * kUnits; i += 128) {
-                    const int row = (i + thread) / kUnits, u = (i + thread) % kUnits * kUnit, at = c * kChunk + row;
-                    if (kChunk * kUnits % 128 && row >= kChunk) break;
+#pragma unroll 4
+                for (int i = lane; i < kChunk * kUnits; i += 32) {
+                    const int row = i / kUnits, u = i % kUnits * kUnit, at = c * kChunk + row;
                     const bool there = at < tokens && first_col + u < a.v_dim;
                     copy_16(smem_u32(values) + row * kPitch + u * (int)sizeof(T), there ? vp + at * a.ldv + u : vp, there ? 16 : 0);
                 }
             } else {
-                for (int i = thread; i < kChunk * Stage::kValues; i += 128) {
+                for (int i = lane; i < kChunk * Stage::kValues; i += 32) {
                     const int row = i / Stage::kValues, u = i % Stage::kValues, at = c * kChunk + row;
                     reinterpret_cast<T*>(values + row * kPitch)[u] = at < tokens && first_col + u < a.v_dim ? vp[at * a.ldv + u] : from_float<T>(0.f);
                 }
@@ -554,10 +580,15 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
     uint8_t* hands = smem + Stage::kStages * Stage::kBytes;
     float4* told = reinterpret_cast<float4*>(hands + 2 * Stage::kHand + ((carries ? 0 : 4) + tile * KS) * 2048);
     const int meet = (carries ? 1 : 5) + tile;
-    struct Hand { uint4* state; float2* scales; float4* fresh; int* walked; };
+    float2* mosts = reinterpret_cast<float2*>(hands + 2 * Stage::kHand + 8 * 2048) + tile * KS * 8 + g;
+    auto tell_most = [&]() {                                     // (true magnitudes; read by the tile's warps in the next chunk)
+        if (KS > 1 && t == 0) mosts[part * 8] = make_float2(most0 * back0, most1 * back1);
+    };
+    if (carries) tell_most();
+    struct Hand { uint4* state; float4* scales; float4* fresh; int* walked; };
     auto hand_of = [&](int c) {
         uint8_t* p = hands + (c & 1) * Stage::kHand;
-        return Hand{reinterpret_cast<uint4*>(p + warp * Stage::kState) + lane, reinterpret_cast<float2*>(p + 4 * Stage::kState + warp * Stage::kScales) + lane,
+        return Hand{reinterpret_cast<uint4*>(p + warp * Stage::kState) + lane, reinterpret_cast<float4*>(p + 4 * Stage::kState + warp * Stage::kScales) + lane,
                     reinterpret_cast<float4*>(p + 4 * (Stage::kState + Stage::kScales) + tile * Stage::kNew) + lane,
                     reinterpret_cast<int*>(p + 4 * (Stage::kState + Stage::kScales) + Stage::kTiles * Stage::kNew) + tile};
     };
@@ -585,14 +616,26 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
         if (walk) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) { S[j][0] *= back0; S[j][1] *= back0; S[j][2] *= back1; S[j][3] *= back1; }
-            by0 = by1 = back0 = back1 = 1.f;
             walk_chunk_tokens<T, KS>(a, S, h, hk, col0, part, t0 + (long long)c * kChunk, min(kChunk, tokens - c * kChunk), told, meet);
-            settle(0.f, 0.f);
+            settle();
+            tell_most();
             return;
         }
+        // the bounds: of what enters the solve, and (its columns below 2^9 each) of V'
+        float value0 = 0.f, value1 = 0.f, held0 = most0 * back0, held1 = most1 * back1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            value0 = fmaxf(value0, fmaxf(fabsf(v[i][0]), fabsf(v[i][1])));
+            value1 = fmaxf(value1, fmaxf(fabsf(v[i][2]), fabsf(v[i][3])));
+        }
+        if (KS > 1) {
+#pragma unroll
+            for (int p = 0; p < KS; ++p) { const float2 f = mosts[p * 8]; held0 = fmaxf(held0, f.x); held1 = fmaxf(held1, f.y); }
+        }
+        const float enter0 = fmaf(F.put_most, quad_max(value0), F.keep_most * held0), enter1 = fmaf(F.put_most, quad_max(value1), F.keep_most * held1);
+        *out.scales = make_float4(back0, back1, 16384.f * enter0, 16384.f * enter1);
         // S^T k
         float r[4][4] = {};
-        *out.scales = make_float2(back0, back1);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             uint32_t hi[4], lo[4], b[2][4];
@@ -640,31 +683,27 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
         }
         uint32_t hi[2][4], lo[2][4];
         float x[4][4] = {}, inv0, inv1;
-        split_rows(v, hi, lo, inv0, inv1);
+        {
+            const float s0 = scale_of<13>(enter0, inv0), s1 = scale_of<13>(enter1, inv1);
+            split_tile(v, s0, s1, hi, lo);
+        }
         times_lower<0, 4>(x, hi, lo, head + kSolveHi + mat_at, kSolveLo - kSolveHi);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { x[i][0] *= inv0; x[i][1] *= inv0; x[i][2] *= inv1; x[i][3] *= inv1; }
         if (part == 0) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) out.fresh[i * 32] = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+            for (int i = 0; i < 4; ++i) out.fresh[i * 32] = make_float4(x[i][0] * inv0, x[i][1] * inv0, x[i][2] * inv1, x[i][3] * inv1);
         }
-        // the state behind the chunk (a scaled key's values are below 2)
-        float add0 = 0.f, add1 = 0.f;
+        // the state behind the chunk: 32 tokens add V' times key values below 2 each
+        const float whole = F.whole;
+        const float f0 = grow<14>(fmaf(0x1p20f * enter0, by0, whole * most0), back0), f1 = grow<14>(fmaf(0x1p20f * enter1, by1, whole * most1), back1);
+        by0 *= f0; by1 *= f1; back0 = inverse_of(by0); back1 = inverse_of(by1);
+        const float keep0 = whole * f0, keep1 = whole * f1;
+        inv0 *= by0; inv1 *= by1;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float2 te = *reinterpret_cast<const float2*>(&F.to_end[8 * i + 2 * t]);
             x[i][0] *= te.x; x[i][1] *= te.y; x[i][2] *= te.x; x[i][3] *= te.y;
-            add0 += fabsf(x[i][0]) + fabsf(x[i][1]); add1 += fabsf(x[i][2]) + fabsf(x[i][3]);
         }
-        add0 = 2.f * quad_sum(add0); add1 = 2.f * quad_sum(add1);
-        const float whole = F.whole;
-        float b0 = fmaf(add0, by0, whole * bound0), b1 = fmaf(add1, by1, whole * bound1);
-        if (__any_sync(0xffffffffu, fmaxf(b0, b1) > 32768.f || (b0 < 16.f && b0 > 0.f) || (b1 < 16.f && b1 > 0.f))) {
-            settle(add0 * by0, add1 * by1);
-            b0 = fmaf(add0, by0, whole * bound0); b1 = fmaf(add1, by1, whole * bound1);
-        }
-        bound0 = b0; bound1 = b1;
-        split_tile(x, by0, by1, hi, lo);
+        split_tile(x, inv0, inv1, hi, lo);
 #pragma unroll
         for (int j = 0; j < 8; j += 4) {
             float add[4][4] = {};
@@ -691,8 +730,10 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) S[j + i][k] = fmaf(whole, S[j + i][k], add[i][k]);
+                for (int k = 0; k < 4; ++k) S[j + i][k] = fmaf(k >> 1 ? keep1 : keep0, S[j + i][k], add[i][k]);
         }
+        largest();
+        tell_most();
     };
 
     // The outputs of chunk c; the warps of a tile share its tokens evenly.
@@ -722,7 +763,7 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
                 for (int i = 0; i < 4; ++i) mma_f16(o[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
             }
         }
-        const float2 back = *in.scales;
+        const float4 back = *in.scales;
 #pragma unroll
         for (int i = 0; i < 4; ++i) { o[i][0] *= back.x; o[i][1] *= back.x; o[i][2] *= back.y; o[i][3] *= back.y; }
         if (KS > 1) {
@@ -737,7 +778,10 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
             const float4 f = in.fresh[i * 32];
             x[i][0] = f.x; x[i][1] = f.y; x[i][2] = f.z; x[i][3] = f.w;
         }
-        split_rows(x, hi, lo, inv0, inv1);
+        {
+            const float s0 = scale_of<13>(back.z, inv0), s1 = scale_of<13>(back.w, inv1);
+            split_tile(x, s0, s1, hi, lo);
+        }
         constexpr int kMine = 4 / KS;
         auto outputs = [&](auto from) {
             constexpr int FROM = decltype(from)::value;
@@ -774,19 +818,20 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
         else outputs(std::integral_constant<int, KS == 4 ? 3 : 0>());
     };
 
-    if (!carries) fetch(0);
+    if (fetches) fetch(0);
     for (int c = 0; c <= chunks; ++c) {
-        if (!carries) copies_wait<0>();
+        if (fetches) copies_wait<0>();
         __syncthreads();                                        // chunk c is there, and what is handed over of chunk c - 1
         if (carries) {
             if (c < chunks) carry(c);
-        } else {
-            if (Stage::kStages == 3) fetch(c + 1);
+        } else if (!fetches) {
             if (c > 0) put_out(c - 1);
+        } else if (Stage::kStages == 3) {
+            fetch(c + 1);
         }
         if (Stage::kStages == 2) {
             __syncthreads();                                    // chunk c - 1 is done with
-            if (!carries) fetch(c + 1);
+            if (fetches) fetch(c + 1);
         }
     }
     if (slot < 0 || !carries) return;
@@ -841,7 +886,7 @@ static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
     cfg.dynamicSmemBytes = sizeof(PrepareSmem<DKP, sizeof(T) == 4>);
     CSB_CUDA((cudaFuncSetAttribute(csb_delta_prepare_kernel<T, DKP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
     CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_prepare_kernel<T, DKP>, a, w)));
-    cfg.gridDim = dim3((unsigned)((int64_t)a.sequences * a.v_heads * w.groups)); cfg.blockDim = dim3(256);
+    cfg.gridDim = dim3((unsigned)((int64_t)a.sequences * a.v_heads * w.groups)); cfg.blockDim = dim3(288);
     cfg.dynamicSmemBytes = Stage::kSmem;
     CSB_CUDA((cudaFuncSetAttribute(csb_delta_chunk_kernel<T, KS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
     CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_chunk_kernel<T, KS>, a, w)));
