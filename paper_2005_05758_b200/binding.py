@@ -337,91 +337,43 @@ for _f in ("csb_spmm_adapters", "csb_gated_delta_forward", "csb_gated_delta_step
     getattr(lib, _f).restype = C.c_int
 
 
-def _value_types():
+_types = None                              # torch's types, as _csb_py takes them
+
+
+def _looked_at(stream) -> tuple:
+    """(torch's types, current device or -1, stream): what the tensors of a call are compared with, and where it goes."""
+    global _types
     import torch
-    return {torch.float32: CSB_F32, torch.float16: CSB_F16, torch.bfloat16: CSB_BF16}
+    if _types is None:
+        _types = (torch.float32, torch.float16, torch.bfloat16, torch.int32, torch.uint8)
+    if _current is None and not torch.cuda.is_available():
+        return _types, -1, 0                # (no tensor is on device -1)
+    st = _stream(stream)
+    return _types, _current[1]() if _current is not None else torch.cuda.current_device(), st
 
 
-def _tensor(name, t, dtype, shape, where=None, inner=None):
-    """Refuses a tensor that the library would read wrongly: type, sizes (None: any), device, and that its last `inner`
-    dimensions lie behind one another (None: all of them)."""
+def _scratch(device: int, stream):
+    """Makes a workspace of torch's allocator that outlives the work queued on `stream`."""
     import torch
-    if not isinstance(t, torch.Tensor):
-        raise TypeError("%s: a torch tensor is expected, got %s" % (name, type(t).__name__))
-    if t.dtype != dtype:
-        raise TypeError("%s: %s is expected, got %s" % (name, dtype, t.dtype))
-    if t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
-        raise ValueError("%s: shape %s is expected, got %s" % (name, tuple("any" if w is None else w for w in shape), tuple(t.shape)))
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError("%s is on %s: the current CUDA device is expected" % (name, t.device))
-    if where is not None and t.device != where:
-        raise ValueError("%s is on %s, the other tensors on %s" % (name, t.device, where))
-    step, strides = 1, t.stride()
-    for d in range(t.dim() - 1, (0 if inner is None else t.dim() - inner) - 1, -1):
-        if t.shape[d] != 1 and strides[d] != step and t.numel():
-            raise ValueError("%s: its last %d dimensions must be contiguous, strides are %s" % (name, t.dim() if inner is None else inner, strides))
-        step *= t.shape[d]
-    return t
 
-
-def _scratch(nbytes: int, given, device, stream):
-    """The caller's workspace, or one of torch's allocator that outlives the work queued on `stream`."""
-    import torch
-    if given is not None:
-        if not given.is_cuda or given.device != device or not given.is_contiguous():
-            raise ValueError("workspace: a contiguous tensor on %s is expected" % device)
-        return given, given.numel() * given.element_size()
-    buf = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
-    if stream is not None:
-        st = _stream(stream)
-        if st != torch.cuda.current_stream(device).cuda_stream:
-            buf.record_stream(torch.cuda.ExternalStream(st or 0, device=device))
-    return buf, buf.numel()
+    def make(nbytes):
+        buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        if stream is not None:
+            st = _stream(stream)
+            if st != torch.cuda.current_stream(device).cuda_stream:
+                buf.record_stream(torch.cuda.ExternalStream(st or 0, device=device))
+        return buf
+    return make
 
 
 def csb_spmm_adapters(A: CsbMatrix, X, Y, down, up, which, ranks=None, scales=None, workspace=None, stream=None) -> None:
     """Y[b] = A . X[b] + scales[a] * up[a] @ (down[a] @ X[b]) with a = which[b] (none where a is outside 0 .. len(down) - 1).
 
     X float32 [batch, cols], Y float32 [batch, rows]; down [count, rank, cols] and up [count, rows, rank] of one type
-    (float32, float16 or bfloat16); which int32 [batch]; ranks int32 [count], scales float32 [count] (see csb.h)."""
-    import torch
-    types = _value_types()
-    if down.dtype not in types:
-        raise TypeError("down: float32, float16 or bfloat16 is expected, got %s" % down.dtype)
-    rows, cols = A.shape
-    _tensor("X", X, torch.float32, (None, cols), inner=1)
-    _tensor("down", down, down.dtype, (None, None, cols), X.device)
-    batch, (count, rank, _) = X.shape[0], down.shape
-    _tensor("Y", Y, torch.float32, (batch, rows), X.device, inner=1)
-    _tensor("up", up, down.dtype, (count, rows, rank), X.device)
-    _tensor("which", which, torch.int32, (batch,), X.device)
-    if ranks is not None:
-        _tensor("ranks", ranks, torch.int32, (count,), X.device)
-    if scales is not None:
-        _tensor("scales", scales, torch.float32, (count,), X.device)
-    buf, size = _scratch(int(lib.csb_adapters_workspace_bytes(A.handle, batch, rank)), workspace, X.device, stream)
-    _check(lib.csb_spmm_adapters(A.handle, _ptr(X), X.stride(0) if batch > 1 else cols, batch, _ptr(Y), Y.stride(0) if batch > 1 else rows,
-                                 types[down.dtype], count, rank, _ptr(down), _ptr(up), _ptr(which), _ptr(ranks), _ptr(scales), _ptr(buf), size,
-                                 _stream(stream)))
-
-
-def _delta_shape(q, k, v, g, beta, o, state, sequences, scale):
-    import torch
-    types = _value_types()
-    if q.dtype not in types:
-        raise TypeError("q: float32, float16 or bfloat16 is expected, got %s" % q.dtype)
-    _tensor("q", q, q.dtype, (None, None, None), inner=2)
-    T, Hk, dk = q.shape
-    _tensor("k", k, q.dtype, (T, Hk, dk), q.device, inner=2)
-    _tensor("v", v, q.dtype, (T, None, None), q.device, inner=2)
-    Hv, dv = v.shape[1:]
-    _tensor("g", g, torch.float32, (T, Hv), q.device, inner=1)
-    _tensor("beta", beta, torch.float32, (T, Hv), q.device, inner=1)
-    _tensor("o", o, q.dtype, (T, Hv, dv), q.device, inner=2)
-    if state is not None:
-        _tensor("state", state, torch.float32, (None, Hv, dk, dv), q.device)
-    ld = [t.stride(0) if T > 1 else t[0].numel() if T else t.shape[1] * (t.shape[2] if t.dim() == 3 else 1) for t in (q, k, v, g, beta, o)]
-    return csb_delta_shape_t(T, 0 if state is None else state.shape[0], sequences, Hk, Hv, dk, dv, types[q.dtype], *ld, scale or 0.0)
+    (float32, float16 or bfloat16); which int32 [batch]; ranks int32 [count], scales float32 [count] (see csb.h); workspace
+    uint8 (allocated when not given)."""
+    types, device, st = _looked_at(stream)
+    _check(_csb_py.adapters(_ADAPTERS, types, device, _scratch(device, stream), A, X, Y, down, up, which, ranks, scales, workspace, st))
 
 
 def csb_gated_delta_forward(q, k, v, g, beta, o, state=None, seq_begin=None, slot=None, fresh=None, scale=None, flags: int = 0, workspace=None,
@@ -430,29 +382,25 @@ def csb_gated_delta_forward(q, k, v, g, beta, o, state=None, seq_begin=None, slo
 
     q, k [tokens, k_heads, k_dim], v, o [tokens, v_heads, v_dim] (float32, float16 or bfloat16); g, beta float32 [tokens,
     v_heads]; state float32 [slots, v_heads, k_dim, v_dim]; seq_begin int32 [sequences + 1] (None: one sequence of all
-    tokens); slot int32 [sequences]; fresh uint8 [sequences].  scale None stands for 1 / sqrt(k_dim)."""
-    import torch
-    n = 1 if seq_begin is None else _tensor("seq_begin", seq_begin, torch.int32, (None,)).shape[0] - 1
-    if n < 0:
-        raise ValueError("seq_begin: sequences + 1 entries are expected, got none")
-    shape = _delta_shape(q, k, v, g, beta, o, state, n, scale)
-    if slot is not None:
-        _tensor("slot", slot, torch.int32, (n,), q.device)
-    if fresh is not None:
-        _tensor("fresh", fresh, torch.uint8, (n,), q.device)
-    buf, size = _scratch(int(lib.csb_gated_delta_workspace_bytes(C.byref(shape))), workspace, q.device, stream)
-    _check(lib.csb_gated_delta_forward(C.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(o), _ptr(state), _ptr(seq_begin), _ptr(slot),
-                                       _ptr(fresh), _ptr(buf), size, flags, _stream(stream)))
+    tokens); slot int32 [sequences]; fresh uint8 [sequences].  scale None stands for 1 / sqrt(k_dim); workspace uint8
+    (allocated when not given)."""
+    types, device, st = _looked_at(stream)
+    _check(_csb_py.delta(_DELTA_FORWARD, types, device, _scratch(device, stream), q, k, v, g, beta, o, state, seq_begin, slot, fresh, scale, flags, workspace,
+                         st))
 
 
 def csb_gated_delta_step(q, k, v, g, beta, o, state, slot=None, scale=None, flags: int = 0, stream=None) -> None:
     """The gated delta rule for one token of each of q.shape[0] sequences: tensors as for csb_gated_delta_forward, the
     states in slots of `state` (slot int32 [tokens], None: slot i for token i; a negative one leaves its token out)."""
-    import torch
-    shape = _delta_shape(q, k, v, g, beta, o, state, q.shape[0], scale)
-    if slot is not None:
-        _tensor("slot", slot, torch.int32, (q.shape[0],), q.device)
-    _check(lib.csb_gated_delta_step(C.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(o), _ptr(state), _ptr(slot), flags, _stream(stream)))
+    types, device, st = _looked_at(stream)
+    _check(_csb_py.delta(_DELTA_STEP, types, device, None, q, k, v, g, beta, o, state, None, slot, None, scale, flags, None, st))
+
+
+#: (workspace size, function) addresses that the native marshalling calls.
+_ADAPTERS, _DELTA_FORWARD, _DELTA_STEP = (
+    (C.cast(getattr(lib, w), C.c_void_p).value if w else 0, C.cast(getattr(lib, f), C.c_void_p).value)
+    for w, f in (("csb_adapters_workspace_bytes", "csb_spmm_adapters"), ("csb_gated_delta_workspace_bytes", "csb_gated_delta_forward"),
+                 ("", "csb_gated_delta_step")))
 
 
 # shorter aliases

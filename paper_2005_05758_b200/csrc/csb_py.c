@@ -8,7 +8,7 @@
 
 enum { kMaxList = 64 };
 
-static PyObject *s_data_ptr, *s_shape, *s_stride, *s_handle, *s_value, *s_zero;
+static PyObject *s_data_ptr, *s_shape, *s_stride, *s_handle, *s_value, *s_zero, *s_dtype, *s_device, *s_get_device;
 
 /* Address of a torch tensor (data_ptr()) or of a numpy array (its buffer); None is NULL. */
 static int address(PyObject* o, void** out) {
@@ -148,9 +148,215 @@ static PyObject* py_recurrent(PyObject* self, PyObject* const* a, Py_ssize_t n) 
     return PyLong_FromLong(rc);
 }
 
+/* ---- calls whose tensors are looked at before the library gets their addresses ---- */
+
+enum { kMaxDim = 4 };
+typedef struct { void* ptr; int64_t size[kMaxDim], stride[kMaxDim]; } Tensor;
+
+static int tuple_of(PyObject* t, int n, int64_t* out) {
+    for (int i = 0; i < n; ++i) {
+        out[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
+        if (out[i] == -1 && PyErr_Occurred()) return -1;
+    }
+    return 0;
+}
+static int whole_number(PyObject* o, PyObject* method, int64_t* out) {
+    PyObject* v = PyObject_CallMethodNoArgs(o, method);
+    if (!v) return -1;
+    *out = PyLong_AsLongLong(v);
+    Py_DECREF(v);
+    return *out == -1 && PyErr_Occurred() ? -1 : 0;
+}
+/* Which of the `n` types in the tuple `types` a tensor has; -1 with an error set. */
+static int type_of(PyObject* o, const char* name, PyObject* types, int n) {
+    PyObject* d = PyObject_GetAttr(o, s_dtype);
+    if (!d) { PyErr_Clear(); PyErr_Format(PyExc_TypeError, "%s: a torch tensor is expected, got %s", name, Py_TYPE(o)->tp_name); return -1; }
+    for (int i = 0; i < n; ++i)
+        if (d == PyTuple_GET_ITEM(types, i)) { Py_DECREF(d); return i; }
+    PyErr_Format(PyExc_TypeError, "%s: float32, float16 or bfloat16 is expected, got %S", name, d);
+    Py_DECREF(d);
+    return -1;
+}
+/* Refuses a tensor that the library would read wrongly: type, sizes (want[i] < 0: any), device, and that its last `inner`
+ * dimensions lie behind one another. */
+static int tensor_of(PyObject* o, const char* name, PyObject* dtype, int dims, const int64_t* want, int inner, long device, Tensor* t) {
+    PyObject* d = PyObject_GetAttr(o, s_dtype);
+    if (!d) { PyErr_Clear(); PyErr_Format(PyExc_TypeError, "%s: a torch tensor is expected, got %s", name, Py_TYPE(o)->tp_name); return -1; }
+    if (d != dtype) PyErr_Format(PyExc_TypeError, "%s: %S is expected, got %S", name, dtype, d);
+    Py_DECREF(d);
+    if (PyErr_Occurred()) return -1;
+    PyObject* s = PyObject_GetAttr(o, s_shape);
+    if (!s) return -1;
+    int bad = !PyTuple_Check(s) || PyTuple_GET_SIZE(s) != dims;
+    if (!bad && tuple_of(s, dims, t->size)) { Py_DECREF(s); return -1; }
+    for (int i = 0; i < dims && !bad; ++i) bad = want[i] >= 0 && want[i] != t->size[i];
+    if (bad) {
+        PyObject* w = PyTuple_New(dims);
+        for (int i = 0; w && i < dims; ++i) PyTuple_SET_ITEM(w, i, want[i] < 0 ? PyUnicode_FromString("any") : PyLong_FromLongLong(want[i]));
+        if (w) PyErr_Format(PyExc_ValueError, "%s: shape %S is expected, got %S", name, w, s);
+        Py_XDECREF(w);
+    }
+    Py_DECREF(s);
+    if (bad) return -1;
+    int64_t at;
+    if (whole_number(o, s_get_device, &at)) return -1;
+    if (at != device || at < 0) {
+        PyObject* v = PyObject_GetAttr(o, s_device);
+        if (v) PyErr_Format(PyExc_ValueError, "%s is on %S: the current CUDA device is expected", name, v);
+        Py_XDECREF(v);
+        return -1;
+    }
+    s = PyObject_CallMethodNoArgs(o, s_stride);
+    if (!s) return -1;
+    if (!PyTuple_Check(s) || PyTuple_GET_SIZE(s) != dims || tuple_of(s, dims, t->stride)) {
+        Py_DECREF(s);
+        if (!PyErr_Occurred()) PyErr_Format(PyExc_TypeError, "%s: strides", name);
+        return -1;
+    }
+    int64_t step = 1;
+    int empty = 0;
+    for (int i = 0; i < dims; ++i) empty |= t->size[i] == 0;
+    for (int i = dims - 1; i >= dims - inner; --i) {
+        if (!empty && t->size[i] != 1 && t->stride[i] != step) {
+            PyErr_Format(PyExc_ValueError, "%s: its last %d dimensions must be contiguous, strides are %S", name, inner, s);
+            Py_DECREF(s);
+            return -1;
+        }
+        step *= t->size[i];
+    }
+    Py_DECREF(s);
+    return address(o, &t->ptr);
+}
+/* Elements from a row to the next, as the library takes them: of a single row any will do. */
+static int64_t row_step(const Tensor* t, int dims) {
+    int64_t row = 1;
+    for (int i = 1; i < dims; ++i) row *= t->size[i];
+    return t->size[0] > 1 ? t->stride[0] : row;
+}
+/* The caller's workspace (None: what make(bytes) returns, kept alive by *keep). */
+static int scratch_of(PyObject* given, PyObject* make, int64_t bytes, long device, PyObject* uint8, void** ptr, int64_t* size, PyObject** keep) {
+    *keep = NULL; *ptr = NULL; *size = 0;
+    if (given == Py_None) {
+        if (bytes <= 0) return 0;
+        PyObject* n = PyLong_FromLongLong(bytes);
+        if (!n) return -1;
+        *keep = PyObject_CallOneArg(make, n);
+        Py_DECREF(n);
+        *size = bytes;
+        return *keep ? address(*keep, ptr) : -1;
+    }
+    const int64_t any = -1;
+    Tensor t;
+    if (tensor_of(given, "workspace", uint8, 1, &any, 1, device, &t)) return -1;
+    *ptr = t.ptr; *size = t.size[0];
+    return 0;
+}
+
+/* Layout of csb.h's csb_delta_shape_t. */
+typedef struct {
+    int64_t tokens, slots;
+    int32_t sequences, k_heads, v_heads, k_dim, v_dim, dtype;
+    int64_t ldq, ldk, ldv, ldg, ldb, ldo;
+    float scale;
+} DeltaShape;
+static const int32_t kValueTypes[3] = {0, 1, 3};      /* CSB_F32, CSB_F16, CSB_BF16 */
+
+/* delta(functions, types, device, make, q, k, v, g, beta, o, state, seq_begin, slot, fresh, scale, flags, workspace, stream)
+ * functions: (workspace bytes, forward) or (0, step); types: torch's (float32, float16, bfloat16, int32, uint8). */
+static PyObject* py_delta(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *f_ws, *f, *st, *ws;
+    int64_t ws_size;
+    unsigned flags;
+    int rc;
+    if (arity(n, 18) || pointer(PyTuple_GET_ITEM(a[0], 0), &f_ws) || pointer(PyTuple_GET_ITEM(a[0], 1), &f) || flag_bits(a[15], &flags) || pointer(a[17], &st)) return NULL;
+    PyObject *types = a[1], *f32 = PyTuple_GET_ITEM(types, 0), *i32 = PyTuple_GET_ITEM(types, 3), *u8 = PyTuple_GET_ITEM(types, 4);
+    const long device = PyLong_AsLong(a[2]);
+    const int kind = type_of(a[4], "q", types, 3);
+    if (kind < 0 || (device == -1 && PyErr_Occurred())) return NULL;
+    PyObject* type = PyTuple_GET_ITEM(types, kind);
+    Tensor q, k, v, g, b, o, S = {0}, begin = {0}, slot = {0}, fresh = {0};
+    const int64_t any3[3] = {-1, -1, -1}, any1 = -1;
+    if (tensor_of(a[4], "q", type, 3, any3, 2, device, &q)) return NULL;
+    if (tensor_of(a[5], "k", type, 3, q.size, 2, device, &k)) return NULL;
+    const int64_t T = q.size[0], want_v[3] = {T, -1, -1};
+    if (tensor_of(a[6], "v", type, 3, want_v, 2, device, &v)) return NULL;
+    const int64_t want_g[2] = {T, v.size[1]}, want_S[4] = {-1, v.size[1], q.size[2], v.size[2]};
+    if (tensor_of(a[7], "g", f32, 2, want_g, 1, device, &g) || tensor_of(a[8], "beta", f32, 2, want_g, 1, device, &b) ||
+        tensor_of(a[9], "o", type, 3, v.size, 2, device, &o) || (a[10] != Py_None && tensor_of(a[10], "state", f32, 4, want_S, 4, device, &S)))
+        return NULL;
+    int64_t sequences = f_ws ? 1 : T;
+    if (a[11] != Py_None) {
+        if (tensor_of(a[11], "seq_begin", i32, 1, &any1, 1, device, &begin)) return NULL;
+        sequences = begin.size[0] - 1;
+        if (sequences < 0) { PyErr_SetString(PyExc_ValueError, "seq_begin: sequences + 1 entries are expected, got none"); return NULL; }
+    }
+    if (a[12] != Py_None && tensor_of(a[12], "slot", i32, 1, &sequences, 1, device, &slot)) return NULL;
+    if (a[13] != Py_None && tensor_of(a[13], "fresh", u8, 1, &sequences, 1, device, &fresh)) return NULL;
+    double scale = 0.0;
+    if (a[14] != Py_None) {
+        scale = PyFloat_AsDouble(a[14]);
+        if (scale == -1.0 && PyErr_Occurred()) return NULL;
+    }
+    const int64_t most = INT32_MAX;
+    if (sequences > most || q.size[1] > most || v.size[1] > most || q.size[2] > most || v.size[2] > most) {
+        PyErr_SetString(PyExc_ValueError, "a size is above 2^31 - 1");
+        return NULL;
+    }
+    DeltaShape s = {T, S.size[0], (int32_t)sequences, (int32_t)q.size[1], (int32_t)v.size[1], (int32_t)q.size[2], (int32_t)v.size[2], kValueTypes[kind],
+                    row_step(&q, 3), row_step(&k, 3), row_step(&v, 3), row_step(&g, 2), row_step(&b, 2), row_step(&o, 3), (float)scale};
+    PyObject* keep = NULL;
+    if (f_ws && scratch_of(a[16], a[3], ((int64_t (*)(const DeltaShape*))f_ws)(&s), device, u8, &ws, &ws_size, &keep)) { Py_XDECREF(keep); return NULL; }
+    Py_BEGIN_ALLOW_THREADS
+    if (f_ws)
+        rc = ((int (*)(const DeltaShape*, void*, void*, void*, void*, void*, void*, void*, void*, void*, void*, void*, int64_t, unsigned, void*))f)(
+            &s, q.ptr, k.ptr, v.ptr, g.ptr, b.ptr, o.ptr, S.ptr, begin.ptr, slot.ptr, fresh.ptr, ws, ws_size, flags, st);
+    else
+        rc = ((int (*)(const DeltaShape*, void*, void*, void*, void*, void*, void*, void*, void*, unsigned, void*))f)(&s, q.ptr, k.ptr, v.ptr, g.ptr, b.ptr, o.ptr,
+                                                                                                                S.ptr, slot.ptr, flags, st);
+    Py_END_ALLOW_THREADS
+    Py_XDECREF(keep);
+    return PyLong_FromLong(rc);
+}
+
+/* adapters(functions, types, device, make, matrix, X, Y, down, up, which, ranks, scales, workspace, stream); functions: (workspace
+ * bytes, product); types as for delta. */
+static PyObject* py_adapters(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *f_ws, *f, *h, *st, *ws;
+    int64_t ws_size, R, Cn;
+    int rc;
+    if (arity(n, 14) || pointer(PyTuple_GET_ITEM(a[0], 0), &f_ws) || pointer(PyTuple_GET_ITEM(a[0], 1), &f) || handle_of(a[4], &h) || size_at(a[4], 0, &R) ||
+        size_at(a[4], 1, &Cn) || pointer(a[13], &st))
+        return NULL;
+    PyObject *types = a[1], *f32 = PyTuple_GET_ITEM(types, 0), *i32 = PyTuple_GET_ITEM(types, 3), *u8 = PyTuple_GET_ITEM(types, 4);
+    const long device = PyLong_AsLong(a[2]);
+    const int kind = type_of(a[7], "down", types, 3);
+    if (kind < 0 || (device == -1 && PyErr_Occurred())) return NULL;
+    PyObject* type = PyTuple_GET_ITEM(types, kind);
+    Tensor X, Y, down, up, which, ranks = {0}, scales = {0};
+    const int64_t want_x[2] = {-1, Cn}, want_down[3] = {-1, -1, Cn};
+    if (tensor_of(a[5], "X", f32, 2, want_x, 1, device, &X) || tensor_of(a[7], "down", type, 3, want_down, 3, device, &down)) return NULL;
+    const int64_t batch = X.size[0], count = down.size[0], rank = down.size[1], want_y[2] = {batch, R}, want_up[3] = {count, R, rank};
+    if (tensor_of(a[6], "Y", f32, 2, want_y, 1, device, &Y) || tensor_of(a[8], "up", type, 3, want_up, 3, device, &up) ||
+        tensor_of(a[9], "which", i32, 1, &batch, 1, device, &which) || (a[10] != Py_None && tensor_of(a[10], "ranks", i32, 1, &count, 1, device, &ranks)) ||
+        (a[11] != Py_None && tensor_of(a[11], "scales", f32, 1, &count, 1, device, &scales)))
+        return NULL;
+    if (batch > INT32_MAX || count > INT32_MAX || rank > INT32_MAX) { PyErr_SetString(PyExc_ValueError, "a size is above 2^31 - 1"); return NULL; }
+    PyObject* keep = NULL;
+    if (scratch_of(a[12], a[3], ((int64_t (*)(void*, int, int))f_ws)(h, (int)batch, (int)rank), device, u8, &ws, &ws_size, &keep)) { Py_XDECREF(keep); return NULL; }
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((int (*)(void*, void*, int64_t, int, void*, int64_t, int, int, int, void*, void*, void*, void*, void*, void*, int64_t, void*))f)(
+        h, X.ptr, row_step(&X, 2), (int)batch, Y.ptr, row_step(&Y, 2), kValueTypes[kind], (int)count, (int)rank, down.ptr, up.ptr, which.ptr, ranks.ptr, scales.ptr,
+        ws, ws_size, st);
+    Py_END_ALLOW_THREADS
+    Py_XDECREF(keep);
+    return PyLong_FromLong(rc);
+}
+
 static PyMethodDef methods[] = {{"spmv", (PyCFunction)(void (*)(void))py_spmv, METH_FASTCALL, NULL},
                                 {"spmm", (PyCFunction)(void (*)(void))py_spmm, METH_FASTCALL, NULL},
                                 {"recurrent", (PyCFunction)(void (*)(void))py_recurrent, METH_FASTCALL, NULL},
+                                {"delta", (PyCFunction)(void (*)(void))py_delta, METH_FASTCALL, NULL},
+                                {"adapters", (PyCFunction)(void (*)(void))py_adapters, METH_FASTCALL, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_csb_py", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
@@ -161,6 +367,10 @@ PyMODINIT_FUNC PyInit__csb_py(void) {
     s_handle = PyUnicode_InternFromString("handle");
     s_value = PyUnicode_InternFromString("value");
     s_zero = PyLong_FromLong(0);
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_device = PyUnicode_InternFromString("device");
+    s_get_device = PyUnicode_InternFromString("get_device");
+    if (!s_dtype || !s_device || !s_get_device) return NULL;
     if (!s_data_ptr || !s_shape || !s_stride || !s_handle || !s_value || !s_zero) return NULL;
     return PyModule_Create(&module);
 }
