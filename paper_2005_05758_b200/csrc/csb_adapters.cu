@@ -3,7 +3,7 @@
 // The shared product is csb_spmm's.  The adapters' part is two kernels around it: csb_adapter_down_kernel takes
 // down_a X[b, :] into the workspace, csb_adapter_up_kernel adds up_a times that to Y.  Requests of one adapter are taken
 // eight at a time (the eight columns of a tensor-core tile), found by every CTA for itself from `which`: nothing is sorted
-// and no order of atomics enters.  Both kernels are bound by reading the adapters once; the arithmetic is in two tf32
+// beforehand and no order of atomics enters.  Both kernels are bound by reading the adapters once; the arithmetic is in two tf32
 // halves of the fp32 operand (22 bits; 16-bit adapters are one such half exactly, fp32 adapters two), fp32 sums.
 #include <algorithm>
 
@@ -16,6 +16,7 @@ namespace csb {
 constexpr int kGroup = 8;               // requests of one adapter that a CTA takes together
 constexpr int kDownThreads = 256, kUpThreads = 256;
 constexpr int kMaxRank = 256;
+constexpr int kGroupWords = 12;         // of a group in the workspace
 constexpr int kScan = 4;                // entries of `which` that a thread looks at between two barriers
 
 struct AdapterArgs {
@@ -24,46 +25,67 @@ struct AdapterArgs {
     const int32_t *which, *ranks;
     const float* scales;
     float* part;                        // [splits][batch][rank_pad]
+    int32_t* groups;                    // [CTAs of a split][kGroupWords]: adapter, requests, which they are; from the first kernel to the second
     long long ldx, ldy;
     int batch, count, rank, rank_pad, rows, cols, splits, split_cols;
+    int by_adapter;                     // how CTAs find their requests (find_group)
 };
 
 struct Group {
     int32_t seen[kScan * (kDownThreads / 32)];
-    int32_t rank_of_b;
+    int32_t rank_of_b, adapter, size;
     int32_t member[kGroup];
 };
 
-// The requests that CTA `b` works for: none unless b's place among the requests of its adapter is a multiple of kGroup,
-// else b and up to kGroup - 1 that follow it.  Returns their number; all threads of the block take part.
+// The entries of `which` from `base` on that a thread looks at, and of those that are `mine` the number in front of each, `before`
+// (those in front of `base`) included; returns the number up to the last entry.  A barrier in the middle.
 template <int NT>
-__device__ int find_group(const AdapterArgs& a, int b, Group& G) {
-    const int mine = a.which[b];
-    if (mine < 0 || mine >= a.count) return 0;
+__device__ __forceinline__ int count_same(Group& G, const int (&theirs)[kScan], int mine, int before, bool (&same)[kScan], int (&at)[kScan]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int before = 0, first = -1, found = 0;
-    for (int base = 0; base < a.batch; base += NT * kScan) {
-        uint32_t same[kScan];
+    uint32_t votes[kScan];
 #pragma unroll
-        for (int i = 0; i < kScan; ++i) {
-            const int j = base + i * NT + (int)threadIdx.x;
-            same[i] = __ballot_sync(0xffffffffu, j < a.batch && a.which[j] == mine);
-            if (lane == 0) G.seen[i * (NT / 32) + warp] = __popc(same[i]);
+    for (int i = 0; i < kScan; ++i) {
+        votes[i] = __ballot_sync(0xffffffffu, theirs[i] == mine);
+        same[i] = votes[i] >> lane & 1u;
+        if (lane == 0) G.seen[i * (NT / 32) + warp] = __popc(votes[i]);
+    }
+    __syncthreads();
+    int total = before;
+#pragma unroll
+    for (int i = 0; i < kScan; ++i)
+        for (int w = 0; w < NT / 32; ++w) {
+            if (w == warp) at[i] = total + __popc(votes[i] & ((1u << lane) - 1u));
+            total += G.seen[i * (NT / 32) + w];
         }
-        __syncthreads();
-        int at[kScan], total = before;
+    return total;
+}
+template <int NT>
+__device__ __forceinline__ void look_at(const AdapterArgs& a, int base, int (&theirs)[kScan]) {
 #pragma unroll
-        for (int i = 0; i < kScan; ++i)
-            for (int w = 0; w < NT / 32; ++w) {
-                if (w == warp) at[i] = total + __popc(same[i] & ((1u << lane) - 1u));
-                total += G.seen[i * (NT / 32) + w];
-            }
-        before = total;
-        if (b >= base + NT * kScan) { __syncthreads(); continue; }
-        if (b >= base) {
+    for (int i = 0; i < kScan; ++i) {
+        const int j = base + i * NT + (int)threadIdx.x;
+        theirs[i] = j < a.batch ? a.which[j] : -1;
+    }
+}
+
+// The requests that CTA `x` works for, their number (0: none) and their adapter; all threads of the block take part.
+// Where most requests are the only ones of their adapter: none unless x's place among the requests of its adapter is a multiple of
+// kGroup, else x and up to kGroup - 1 that follow it.
+template <int NT>
+__device__ int find_group_of_request(const AdapterArgs& a, int x, Group& G) {
+    const int mine = a.which[x];
+    int before = 0, first = -1, found = 0, theirs[kScan], at[kScan];
+    bool same[kScan];
+    look_at<NT>(a, 0, theirs);                                   // (together with the load of `mine`)
+    if (mine < 0 || mine >= a.count) return 0;
+    for (int base = 0; base < a.batch; base += NT * kScan) {
+        if (base) look_at<NT>(a, base, theirs);
+        before = count_same<NT>(G, theirs, mine, before, same, at);
+        if (x >= base + NT * kScan) { __syncthreads(); continue; }
+        if (x >= base) {
 #pragma unroll
             for (int i = 0; i < kScan; ++i)
-                if (base + i * NT + (int)threadIdx.x == b) G.rank_of_b = at[i];
+                if (base + i * NT + (int)threadIdx.x == x) G.rank_of_b = at[i];
             __syncthreads();
             first = G.rank_of_b;
             if (first % kGroup) return 0;
@@ -71,29 +93,86 @@ __device__ int find_group(const AdapterArgs& a, int b, Group& G) {
 #pragma unroll
         for (int i = 0; i < kScan; ++i) {
             const int j = base + i * NT + (int)threadIdx.x;
-            if (j >= b && (same[i] >> lane & 1u) && at[i] - first < kGroup) G.member[at[i] - first] = j;
+            if (j >= x && same[i] && at[i] - first < kGroup) G.member[at[i] - first] = j;
         }
         found = min(before - first, kGroup);
         __syncthreads();
         if (found == kGroup) break;
     }
+    if (threadIdx.x == 0) G.adapter = mine;
+    __syncthreads();
     return found;
+}
+// Where adapters have many requests each: the x-th group when the adapters' groups are counted one adapter after another.
+template <int NT>
+__device__ int find_group_of_adapter(const AdapterArgs& a, int x, Group& G) {
+    extern __shared__ int requests[];                            // of each adapter
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int i = threadIdx.x; i < a.count; i += NT) requests[i] = 0;
+    if (threadIdx.x == 0) G.size = 0;
+    __syncthreads();
+    for (int j = threadIdx.x; j < a.batch; j += NT) {
+        const int w = a.which[j];
+        if (w >= 0 && w < a.count) atomicAdd(&requests[w], 1);
+    }
+    __syncthreads();
+    const int each = (a.count + NT - 1) / NT, lo = min((int)threadIdx.x * each, a.count), hi = min(lo + each, a.count);
+    int sum = 0;
+    for (int i = lo; i < hi; ++i) sum += (requests[i] + kGroup - 1) / kGroup;
+    int upto = sum;                                              // groups up to this thread's last adapter
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int in_front = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += in_front;
+    }
+    if (lane == 31) G.seen[warp] = upto;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) upto += G.seen[w];
+    int at_group = upto - sum;
+    if (x >= at_group && x < upto) {
+        int i = lo;
+        for (int n; x >= at_group + (n = (requests[i] + kGroup - 1) / kGroup); ++i) at_group += n;
+        G.adapter = i;
+        G.rank_of_b = (x - at_group) * kGroup;
+        G.size = min(requests[i] - G.rank_of_b, kGroup);
+    }
+    __syncthreads();
+    const int found = G.size, first = G.rank_of_b, mine = G.adapter;
+    if (!found) return 0;
+    int before = 0, theirs[kScan], at[kScan];
+    bool same[kScan];
+    for (int base = 0; base < a.batch && before < first + found; base += NT * kScan) {
+        look_at<NT>(a, base, theirs);
+        before = count_same<NT>(G, theirs, mine, before, same, at);
+#pragma unroll
+        for (int i = 0; i < kScan; ++i)
+            if (same[i] && at[i] >= first && at[i] < first + kGroup) G.member[at[i] - first] = base + i * NT + (int)threadIdx.x;
+        __syncthreads();
+    }
+    return found;
+}
+template <int NT>
+__device__ int find_group(const AdapterArgs& a, int x, Group& G) {
+    return a.by_adapter ? find_group_of_adapter<NT>(a, x, G) : find_group_of_request<NT>(a, x, G);
 }
 
 __device__ __forceinline__ int rank_of(const AdapterArgs& a, int which) {
     return a.ranks ? min(max(a.ranks[which], 0), a.rank) : a.rank;
 }
 
-// Eight values of a row of `size` from element c on, zeros behind its end.
+// Eight values of a row of `size` from element c on, zeros behind its end and where `there` is false.  (What is not there is
+// read elsewhere in the row and dropped: a branch around a load would wait for it.)
 template <bool VEC, typename T>
 __device__ __forceinline__ void eight(const T* row, int c, int size, bool there, float (&v)[8]) {
     if (VEC) {
-        if (there && c < size) { load_values(row + c, v); return; }            // (size is a multiple of 8)
+        load_values(row + (c < size ? c : 0), v);                // (size is a multiple of 8)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = there && c < size ? v[i] : 0.f;
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = there && c + i < size ? to_float(row[c + i]) : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = to_float(row[min(c + i, size - 1)]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = there && c + i < size ? v[i] : 0.f;
     }
 }
 
@@ -101,14 +180,18 @@ __device__ __forceinline__ void eight(const T* row, int c, int size, bool there,
 // 8t .. 8t + 7 of ranks g and g + 8 and of request g, which are its operands of four steps of eight columns when those are
 // counted in another order, so that every operand comes by wide loads straight from global memory.
 template <typename T, int MT, bool VEC>
-__global__ void __launch_bounds__(kDownThreads) csb_adapter_down_kernel(const AdapterArgs a) {
+__global__ void __launch_bounds__(kDownThreads) csb_adapter_down_kernel(AdapterArgs a) {
     __shared__ Group G;
     __shared__ float sum[kDownThreads / 32][MT * 16 * kGroup];
     pdl_launch_dependents();
     pdl_wait();
-    const int b = blockIdx.x, n = find_group<kDownThreads>(a, b, G);
+    const int n = find_group<kDownThreads>(a, blockIdx.x, G);
+    if (blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < 2 + kGroup) {
+        const int i = threadIdx.x;
+        a.groups[blockIdx.x * kGroupWords + i] = i == 0 ? (n ? G.adapter : 0) : i == 1 ? n : i - 2 < n ? G.member[i - 2] : 0;
+    }
     if (!n) return;
-    const int which = a.which[b], rank = rank_of(a, which), r0 = (int)blockIdx.z * MT * 16;
+    const int which = G.adapter, rank = rank_of(a, which), r0 = (int)blockIdx.z * MT * 16;
     if (r0 >= rank) return;                                      // (the other kernel reads no such part)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const T* down = static_cast<const T*>(a.down) + (size_t)which * a.rank * a.cols;
@@ -128,8 +211,8 @@ __global__ void __launch_bounds__(kDownThreads) csb_adapter_down_kernel(const Ad
         for (int m = 0; m < MT; ++m) {
             const int r = r0 + m * 16 + g;
             float u[8], v[8];
-            eight<VEC>(down + (size_t)r * a.cols, c, c_end, r < rank, u);
-            eight<VEC>(down + (size_t)(r + 8) * a.cols, c, c_end, r + 8 < rank, v);
+            eight<VEC>(down + (size_t)min(r, rank - 1) * a.cols, c, c_end, r < rank, u);
+            eight<VEC>(down + (size_t)min(r + 8, rank - 1) * a.cols, c, c_end, r + 8 < rank, v);
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
                 uint32_t w[4] = {__float_as_uint(u[i]), __float_as_uint(v[i]), __float_as_uint(u[i + 1]), __float_as_uint(v[i + 1])};
@@ -159,70 +242,97 @@ __global__ void __launch_bounds__(kDownThreads) csb_adapter_down_kernel(const Ad
     }
 }
 
-// Y[b, rows] += s_a up_a (sum of the parts).  A warp takes 16 rows at a time; lane 4g + t has ranks 4t .. 4t + 3 of every
-// 16 of rows g and g + 8 (again two steps in an order of their own).
-template <typename T, bool VEC>
+// Y[b, rows] += s_a up_a (sum of the parts).  A warp takes 16 rows at a time, RT times 16 ranks at a time (all of them up to a
+// rank of 64); lane 4g + t has ranks 4t .. 4t + 3 of every 16 of rows g and g + 8 (again two steps in an order of their own).
+// Bound by latency: what a tile needs is loaded a tile ahead, the first one's beside the parts.
+template <typename T, int RT, bool VEC>
 __global__ void __launch_bounds__(kUpThreads) csb_adapter_up_kernel(const AdapterArgs a, int rows_a_cta) {
-    __shared__ Group G;
     __shared__ __align__(16) uint32_t hi[kGroup][kMaxRank + 16], lo[kGroup][kMaxRank + 16];
     pdl_launch_dependents();
     pdl_wait();
-    const int b = blockIdx.x, n = find_group<kUpThreads>(a, b, G);
+    const int32_t* group = a.groups + blockIdx.x * kGroupWords;
+    const int which = group[0], n = group[1];
     if (!n) return;
-    const int which = a.which[b], rank = rank_of(a, which);
+    const int rank = rank_of(a, which);
     if (rank == 0) return;
     const float scale = a.scales ? a.scales[which] : 1.f;
-    for (int i = threadIdx.x; i < kGroup * a.rank_pad; i += kUpThreads) {
-        const int j = i / a.rank_pad, r = i % a.rank_pad;
-        float s = 0.f;
-        if (j < n && r < rank)
-            for (int p = 0; p < a.splits; ++p) s += a.part[((size_t)p * a.batch + G.member[j]) * a.rank_pad + r];
-        split_tf32(s * scale, hi[j][r], lo[j][r]);
-    }
-    __syncthreads();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const T* up = static_cast<const T*>(a.up) + (size_t)which * a.rank * a.rows;
     const int end = min(a.rows, ((int)blockIdx.y + 1) * rows_a_cta);
-    for (int i0 = (int)blockIdx.y * rows_a_cta + warp * 16; i0 < end; i0 += kUpThreads / 2) {
-        float d[4] = {0.f, 0.f, 0.f, 0.f};
-        float y[4];
+    const int j0 = min(2 * t, n - 1), j1 = min(2 * t + 1, n - 1);
+    float* y0 = a.Y + (long long)group[2 + j0] * a.ldy;
+    float* y1 = a.Y + (long long)group[2 + j1] * a.ldy;
+    // (what is not there is read elsewhere in the tensors and dropped)
+    float u[RT][2][4], y[4];
+    auto load_up = [&](int i0, int r0) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int row = i0 + g + (k >> 1) * 8, j = 2 * t + (k & 1);
-            y[k] = row < end && j < n ? a.Y[(long long)G.member[j] * a.ldy + row] : 0.f;
-        }
-        for (int r0 = 0; r0 < rank; r0 += 16) {
-            const int r = r0 + 4 * t;
-            float u[2][4];
+        for (int m = 0; m < RT; ++m)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const int row = i0 + g + 8 * k;
-                const T* p = up + (size_t)row * a.rank + r;
-                if (VEC && row < end && r + 4 <= rank) load_values(p, u[k]);
+                const int r = r0 + 16 * m + 4 * t;
+                const T* p = up + (size_t)min(i0 + g + 8 * k, end - 1) * a.rank;
+                if (VEC) load_values(p + (r < a.rank ? r : 0), u[m][k]);
                 else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) u[k][i] = row < end && r + i < rank ? to_float(p[i]) : 0.f;
+                    for (int i = 0; i < 4; ++i) u[m][k][i] = to_float(p[min(r + i, a.rank - 1)]);
                 }
             }
-            const uint4 h = *reinterpret_cast<const uint4*>(&hi[g][r]), l = *reinterpret_cast<const uint4*>(&lo[g][r]);
-#pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-                uint32_t w[4] = {__float_as_uint(u[0][i]), __float_as_uint(u[1][i]), __float_as_uint(u[0][i + 1]), __float_as_uint(u[1][i + 1])};
-                const uint32_t h0 = i ? h.z : h.x, h1 = i ? h.w : h.y, l0 = i ? l.z : l.x, l1 = i ? l.w : l.y;
-                if (sizeof(T) == 4) {
-                    uint32_t wl[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) split_tf32(__uint_as_float(w[k]), w[k], wl[k]);
-                    mma_tf32(d, wl, h0, h1);
-                }
-                mma_tf32(d, w, l0, l1);
-                mma_tf32(d, w, h0, h1);
-            }
+    };
+    auto load_y = [&](int i0) {
+        const int r0 = min(i0 + g, end - 1), r1 = min(i0 + g + 8, end - 1);
+        y[0] = y0[r0]; y[1] = y1[r0]; y[2] = y0[r1]; y[3] = y1[r1];
+    };
+    int i0 = (int)blockIdx.y * rows_a_cta + warp * 16;
+    if (i0 < end) { load_up(i0, 0); load_y(i0); }
+    for (int i = threadIdx.x; i < kGroup * a.rank_pad; i += kUpThreads) {
+        const int j = i / a.rank_pad, r = i % a.rank_pad;
+        float s = 0.f;
+        if (j < n && r < rank) {
+            const float* p = a.part + (size_t)group[2 + j] * a.rank_pad + r;
+#pragma unroll 8
+            for (int k = 0; k < a.splits; ++k) s += p[(size_t)k * a.batch * a.rank_pad];
         }
+        split_tf32(s * scale, hi[j][r], lo[j][r]);
+    }
+    __syncthreads();
+    for (; i0 < end; i0 += kUpThreads / 2) {
+        float d[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int r0 = 0;;) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int row = i0 + g + (k >> 1) * 8, j = 2 * t + (k & 1);
-            if (row < end && j < n) a.Y[(long long)G.member[j] * a.ldy + row] = y[k] + d[k];
+            for (int m = 0; m < RT; ++m) {
+                const int r = r0 + 16 * m + 4 * t;
+                if (r0 + 16 * m >= rank) break;
+                const uint4 h = *reinterpret_cast<const uint4*>(&hi[g][r]), l = *reinterpret_cast<const uint4*>(&lo[g][r]);
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w[k] = r + i + (k >> 1) < rank ? __float_as_uint(u[m][k & 1][i + (k >> 1)]) : 0u;
+                    const uint32_t h0 = i ? h.z : h.x, h1 = i ? h.w : h.y, l0 = i ? l.z : l.x, l1 = i ? l.w : l.y;
+                    if (sizeof(T) == 4) {
+                        uint32_t wl[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) split_tf32(__uint_as_float(w[k]), w[k], wl[k]);
+                        mma_tf32(d, wl, h0, h1);
+                    }
+                    mma_tf32(d, w, l0, l1);
+                    mma_tf32(d, w, h0, h1);
+                }
+            }
+            r0 += RT * 16;
+            if (r0 >= rank) break;
+            load_up(i0, r0);
+        }
+        const float old[4] = {y[0], y[1], y[2], y[3]};
+        if (i0 + kUpThreads / 2 < end) { load_up(i0 + kUpThreads / 2, 0); load_y(i0 + kUpThreads / 2); }
+        const int r0 = i0 + g, r1 = i0 + g + 8;
+        if (2 * t < n) {
+            if (r0 < end) y0[r0] = old[0] + d[0];
+            if (r1 < end) y0[r1] = old[2] + d[2];
+        }
+        if (2 * t + 1 < n) {
+            if (r0 < end) y1[r0] = old[1] + d[1];
+            if (r1 < end) y1[r1] = old[3] + d[3];
         }
     }
 }
@@ -237,21 +347,27 @@ __global__ void __launch_bounds__(kUpThreads) csb_adapter_up_kernel(const Adapte
     } while (0)
 
 static int rank_pad(int rank) { return (rank + 15) / 16 * 16; }
-// Columns of a split, a multiple of what a CTA takes in one turn: as many splits as give some CTAs to every SM even where
-// all requests of a group of four share an adapter.
-static int split_columns(int64_t cols, int batch) {
+// Groups of requests that a batch may come to: each adapter has one that is not full at most.
+static int most_groups(int batch, int count) { return (int)std::min<int64_t>(batch, (int64_t)count + batch / kGroup); }
+constexpr int kWanted = 592, kWantedUp = 444;   // CTAs that work: four to an SM, three of the second kernel
+// Whether groups are counted by adapter: where that takes half the CTAs or fewer, and the count of each adapter's requests fits
+// in shared memory.  (395 requests of 4 adapters of rank 64 on 4096 x 2048: FIGURES.)
+static bool groups_by_adapter(int batch, int count) { return count <= 4096 && most_groups(batch, count) <= batch / 2; }
+// Columns of a split, a multiple of what a CTA takes in one turn: as many splits as that asks for.
+static int split_columns(int64_t cols, int groups) {
     const int64_t turns = (cols + kDownThreads - 1) / kDownThreads;
-    const int64_t want = std::min<int64_t>(turns, std::max<int64_t>(1, 592 / ((batch + 3) / 4)));
+    const int64_t want = std::min<int64_t>(turns, std::max<int64_t>(1, kWanted / groups));
     return (int)((turns + want - 1) / want * kDownThreads);
 }
-static int64_t workspace_bytes(int64_t cols, int batch, int rank) {
-    const int64_t w = split_columns(cols, batch);
-    return (cols + w - 1) / w * batch * rank_pad(rank) * 4;
+static int64_t workspace_bytes(int64_t cols, int batch, int rank) {           // for any number of adapters
+    const int64_t w = split_columns(cols, std::max(1, batch / kGroup));
+    return ((cols + w - 1) / w * rank_pad(rank) + kGroupWords) * batch * 4;
 }
 
 template <typename... Args>
-static cudaError_t launch(void (*kernel)(Args...), dim3 grid, int threads, void* stream, Args... args) {
+static cudaError_t launch(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, void* stream, Args... args) {
     cudaLaunchConfig_t cfg{};
+    cfg.dynamicSmemBytes = smem;
     cfg.gridDim = grid; cfg.blockDim = dim3((unsigned)threads); cfg.stream = (cudaStream_t)stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -261,11 +377,11 @@ static cudaError_t launch(void (*kernel)(Args...), dim3 grid, int threads, void*
 }
 
 template <typename T, bool VEC>
-static cudaError_t launch_down(const AdapterArgs& a, void* stream) {
+static cudaError_t launch_down(const AdapterArgs& a, unsigned groups, size_t smem, void* stream) {
     const unsigned tiles = (unsigned)(a.rank_pad / 16);
-    if (tiles == 1) return launch<const AdapterArgs>(csb_adapter_down_kernel<T, 1, VEC>, dim3((unsigned)a.batch, (unsigned)a.splits), kDownThreads, stream, a);
-    if (tiles == 2) return launch<const AdapterArgs>(csb_adapter_down_kernel<T, 2, VEC>, dim3((unsigned)a.batch, (unsigned)a.splits), kDownThreads, stream, a);
-    return launch<const AdapterArgs>(csb_adapter_down_kernel<T, 4, VEC>, dim3((unsigned)a.batch, (unsigned)a.splits, (tiles + 3) / 4), kDownThreads, stream, a);
+    const dim3 grid(groups, (unsigned)a.splits, tiles > 2 ? (tiles + 3) / 4 : 1);
+    return launch<AdapterArgs>(tiles == 1 ? csb_adapter_down_kernel<T, 1, VEC> : tiles == 2 ? csb_adapter_down_kernel<T, 2, VEC> : csb_adapter_down_kernel<T, 4, VEC>,
+                               grid, kDownThreads, smem, stream, a);
 }
 
 template <typename T>
@@ -273,16 +389,22 @@ static int adapters_on_device(const csb_matrix* A, AdapterArgs a, void* stream) 
     auto aligned = [](const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; };
     const bool down_vec = a.cols % 8 == 0 && aligned(a.down, 16) && a.ldx % 4 == 0 && aligned(a.X, 16);
     const bool up_vec = a.rank % 4 == 0 && aligned(a.up, 4 * sizeof(T));
-    CSB_CUDA((down_vec ? launch_down<T, true>(a, stream) : launch_down<T, false>(a, stream)));
+    a.by_adapter = groups_by_adapter(a.batch, a.count);
+    const unsigned groups = (unsigned)(a.by_adapter ? most_groups(a.batch, a.count) : a.batch);
+    const size_t smem = a.by_adapter ? (size_t)a.count * 4 : 0;
+    CSB_CUDA((down_vec ? launch_down<T, true>(a, groups, smem, stream) : launch_down<T, false>(a, groups, smem, stream)));
     const int rc = guarded([&] { return product_any(A, a.X, a.ldx, a.batch, a.Y, a.ldy, stream); });
     if (rc != CSB_OK) return rc;
-    // rows of a CTA: fewer where there are few requests, a multiple of what it takes in one turn
-    int rows = kUpThreads / 2;
-    while ((int64_t)a.batch * ((a.rows + rows - 1) / rows) > 8 * 592 && rows < 1024) rows *= 2;
-    while ((a.rows + rows - 1) / rows > 65535) rows *= 2;
-    const dim3 grid((unsigned)a.batch, (unsigned)((a.rows + rows - 1) / rows));
-    CSB_CUDA((up_vec ? launch<const AdapterArgs, int>(csb_adapter_up_kernel<T, true>, grid, kUpThreads, stream, a, rows)
-                    : launch<const AdapterArgs, int>(csb_adapter_up_kernel<T, false>, grid, kUpThreads, stream, a, rows)));
+    // rows of a CTA: a multiple of what it takes in one turn
+    const int64_t turns = (a.rows + kUpThreads / 2 - 1) / (kUpThreads / 2);
+    const int64_t cuts = std::min<int64_t>(turns, std::max<int64_t>(1, kWantedUp / most_groups(a.batch, a.count)));
+    const int rows = (int)((turns + cuts - 1) / cuts * (kUpThreads / 2));
+    const dim3 grid(groups, (unsigned)((a.rows + rows - 1) / rows));
+    const int tiles = a.rank_pad / 16;
+    void (*up)(const AdapterArgs, int) =
+        up_vec ? (tiles == 1 ? csb_adapter_up_kernel<T, 1, true> : tiles == 2 ? csb_adapter_up_kernel<T, 2, true> : csb_adapter_up_kernel<T, 4, true>)
+               : (tiles == 1 ? csb_adapter_up_kernel<T, 1, false> : tiles == 2 ? csb_adapter_up_kernel<T, 2, false> : csb_adapter_up_kernel<T, 4, false>);
+    CSB_CUDA((launch<AdapterArgs, int>(up, grid, kUpThreads, 0, stream, a, rows)));
     return CSB_OK;
 }
 
@@ -320,7 +442,8 @@ int csb_spmm_adapters(const csb_matrix_t* A, const float* X, int64_t ldx, int ba
     AdapterArgs a{};
     a.X = X; a.Y = Y; a.down = down; a.up = up; a.which = which; a.ranks = ranks; a.scales = scales; a.part = static_cast<float*>(workspace);
     a.ldx = ldx; a.ldy = ldy; a.batch = batch; a.count = count; a.rank = rank; a.rank_pad = rank_pad(rank); a.rows = (int)A->rows; a.cols = (int)A->cols;
-    a.split_cols = split_columns(A->cols, batch); a.splits = (a.cols + a.split_cols - 1) / a.split_cols;
+    a.split_cols = split_columns(A->cols, most_groups(batch, count)); a.splits = (a.cols + a.split_cols - 1) / a.split_cols;
+    a.groups = reinterpret_cast<int32_t*>(a.part + (size_t)a.splits * batch * a.rank_pad);
     return dtype == CSB_F32 ? adapters_on_device<float>(A, a, stream) : dtype == CSB_F16 ? adapters_on_device<__half>(A, a, stream)
                                                                                       : adapters_on_device<__nv_bfloat16>(A, a, stream);
 }
