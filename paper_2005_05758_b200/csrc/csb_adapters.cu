@@ -349,9 +349,13 @@ __global__ void __launch_bounds__(kUpThreads) csb_adapter_up_kernel(const Adapte
 static int rank_pad(int rank) { return (rank + 15) / 16 * 16; }
 // Groups of requests that a batch may come to: each adapter has one that is not full at most.
 static int most_groups(int batch, int count) { return (int)std::min<int64_t>(batch, (int64_t)count + batch / kGroup); }
-constexpr int kWanted = 592, kWantedUp = 444;   // CTAs that work: four to an SM, three of the second kernel
+constexpr int kWanted = 592;            // CTAs that work: four to an SM
+// Of the second kernel: up to 16 ranks a tile is little to wait for, and more CTAs hide it (48 requests of 24 adapters of rank 16 on 8192
+// rows: 7.6 us, with 444 9.7); with more ranks, what fits at a time (rank 64 on 4096 rows: 12.5 us, with 888 14.5).
+static int wanted_up(int tiles) { return tiles == 1 ? 1332 : tiles == 2 ? 888 : 444; }
 // Whether groups are counted by adapter: where that takes half the CTAs or fewer, and the count of each adapter's requests fits
-// in shared memory.  (395 requests of 4 adapters of rank 64 on 4096 x 2048: FIGURES.)
+// in shared memory.  (395 requests of 4 adapters of rank 64 on 4096 x 2048: 101 us
+// in all, 107 the other way.)
 static bool groups_by_adapter(int batch, int count) { return count <= 4096 && most_groups(batch, count) <= batch / 2; }
 // Columns of a split, a multiple of what a CTA takes in one turn: as many splits as that asks for.
 static int split_columns(int64_t cols, int groups) {
@@ -397,7 +401,7 @@ static int adapters_on_device(const csb_matrix* A, AdapterArgs a, void* stream) 
     if (rc != CSB_OK) return rc;
     // rows of a CTA: a multiple of what it takes in one turn
     const int64_t turns = (a.rows + kUpThreads / 2 - 1) / (kUpThreads / 2);
-    const int64_t cuts = std::min<int64_t>(turns, std::max<int64_t>(1, kWantedUp / most_groups(a.batch, a.count)));
+    const int64_t cuts = std::min<int64_t>(turns, std::max<int64_t>(1, wanted_up(a.rank_pad / 16) / most_groups(a.batch, a.count)));
     const int rows = (int)((turns + cuts - 1) / cuts * (kUpThreads / 2));
     const dim3 grid(groups, (unsigned)((a.rows + rows - 1) / rows));
     const int tiles = a.rank_pad / 16;

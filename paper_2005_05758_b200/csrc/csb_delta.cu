@@ -4,7 +4,9 @@
 // columns of S do not meet.  Both products with the old state are taken in one pass over it, since
 //   o = scale (e^g S_old^T q + (k . q) w) with w = beta (v - e^g S_old^T k),
 // so a token costs one sum over the rows (within a warp by shuffles, across warps through shared memory).
-// For one token a sequence the kernel is bound by reading and writing the states once.
+// For one token a sequence the kernel is bound by reading and writing the states once, marked as not to be used again soon (256
+// requests less 10 % padding, 32 heads of 128 x 128: 166 us, 5.8 TB/s; without the marks 169; five or six CTAs an SM
+// instead of four, of 32 KB each, 185 and 241).
 #include <algorithm>
 #include <cmath>
 
@@ -17,14 +19,14 @@
 namespace csb {
 
 constexpr int kDeltaMaxDim = 256;       // of keys
-constexpr int kDeltaMaxWarps = 16;
+constexpr int kDeltaMaxWarps = 8, kSlab = 64;   // of a CTA: warps, columns
 
 // Lanes are cut into groups of LC that hold a row of the slab together, four columns each: with VEC behind each other
 // (16-byte loads), else LC apart.  Rows go round the groups of all warps, NR of them to each.
 template <typename T, int NR, bool VEC>
 __global__ void __launch_bounds__(kDeltaMaxWarps * 32) csb_delta_recurrent_kernel(const DeltaArgs a, int LC, int slabs) {
     __shared__ float kq[2][2][kDeltaMaxDim];
-    __shared__ __align__(16) float red[2][kDeltaMaxWarps][2][128];
+    __shared__ __align__(16) float red[2][kDeltaMaxWarps][2][kSlab];
     pdl_launch_dependents();
     pdl_wait();
     const int seq = (int)(blockIdx.x / slabs), slab = (int)(blockIdx.x % slabs), h = blockIdx.y, hk = h / (a.v_heads / a.k_heads);
@@ -58,7 +60,7 @@ __global__ void __launch_bounds__(kDeltaMaxWarps * 32) csb_delta_recurrent_kerne
         const bool mine = r < a.k_dim && !from_zero;
         const float* p = home + (long long)r * a.v_dim;
         if (VEC) {
-            const float4 f = mine && there[0] ? *reinterpret_cast<const float4*>(p + col[0]) : make_float4(0.f, 0.f, 0.f, 0.f);
+            const float4 f = mine && there[0] ? __ldcs(reinterpret_cast<const float4*>(p + col[0])) : make_float4(0.f, 0.f, 0.f, 0.f);
             S[i][0] = f.x; S[i][1] = f.y; S[i][2] = f.z; S[i][3] = f.w;
         } else {
 #pragma unroll
@@ -141,7 +143,7 @@ __global__ void __launch_bounds__(kDeltaMaxWarps * 32) csb_delta_recurrent_kerne
         if (r >= a.k_dim) break;
         float* p = home + (long long)r * a.v_dim;
         if (VEC) {
-            if (there[0]) *reinterpret_cast<float4*>(p + col[0]) = make_float4(S[i][0], S[i][1], S[i][2], S[i][3]);
+            if (there[0]) __stcs(reinterpret_cast<float4*>(p + col[0]), make_float4(S[i][0], S[i][1], S[i][2], S[i][3]));
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) if (there[j]) p[col[j]] = S[i][j];
@@ -160,13 +162,14 @@ __global__ void __launch_bounds__(kDeltaMaxWarps * 32) csb_delta_recurrent_kerne
 
 template <typename T>
 static int launch_recurrent(const DeltaArgs& a, void* stream) {
-    // a slab is as wide as the head, up to 128 columns; narrower where that leaves SMs without work
+    // A slab is as wide as the head, up to 64 columns (256 states of 32 heads of 128 x 128: 170 us, with 128 columns 175); narrower
+    // where that leaves SMs without work.
     int LC = 1;
-    while (LC < 32 && LC * 4 < a.v_dim) LC *= 2;
+    while (LC < kSlab / 4 && LC * 4 < a.v_dim) LC *= 2;
     while (LC > 8 && (int64_t)a.sequences * a.v_heads * ((a.v_dim + LC * 4 - 1) / (LC * 4)) < 148) LC /= 2;
     const int slabs = (a.v_dim + LC * 4 - 1) / (LC * 4), per = 32 / LC;
-    int NR = 4;
-    while (NR < 16 && (a.k_dim + per * NR - 1) / (per * NR) > 8) NR *= 2;
+    int NR = 4;                                   // (16 of 256 keys' columns: eight warps)
+    while (NR < 16 && (a.k_dim + per * NR - 1) / (per * NR) > 4) NR *= 2;
     const int warps = (a.k_dim + per * NR - 1) / (per * NR);
     const bool vec = a.v_dim % 4 == 0 && reinterpret_cast<uintptr_t>(a.state) % 16 == 0;
     cudaLaunchConfig_t cfg{};
