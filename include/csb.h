@@ -389,8 +389,10 @@ int csb_spmm_adapters(const csb_matrix_t* A, const float* X, int64_t ldx, int ba
  *           out: its outputs and states stay as they are.  So does the state of a sequence without tokens.
  *   fresh   device, uint8 [sequences] or NULL: sequences whose byte is not zero start from a state of zeros, whatever the slot holds.
  *   workspace  device, csb_gated_delta_workspace_bytes(shape) bytes of scratch, caller-owned, 16-byte aligned: two calls
- *           that may overlap on the GPU, or two captured graphs, need one each.
- * States, sums and decays are fp32; results are bit-reproducible.  The sizes are all the host looks at: no call
+ *           that may overlap on the GPU, or two captured graphs, need one each.  Its first int32 is 0 behind a call that went
+ *           well; 1 says that a bulk copy did not come within a second, and the outputs are then unspecified.
+ * States, sums and decays are fp32.  Sequences of a forward call that go in chunks of tokens on tensor cores hold what is multiplied
+ * to 2^-22 of the largest value of its row: of a query or key of a token, of a state's column.  Results are bit-reproducible.  The sizes are all the host looks at: no call
  * allocates or synchronises, and all may be captured.  Calls that share slots must be ordered.  All pointers are on the
  * current device.
  * Errors: INVALID_ARG (null, sizes, scale, flags, workspace too small), SHAPE (heads that do not divide, short strides, a step

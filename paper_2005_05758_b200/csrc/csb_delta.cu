@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(kDeltaMaxWarps * 32) csb_delta_recurrent_kerne
         slot = delta_slot(a, seq);
         if (slot < 0) return;
     }
-    if (t0 >= t1) return;
+    if (t0 >= t1 || t1 - t0 > a.longest) return;
     float S[NR][4];
     float* home = a.state + ((slot < 0 ? 0 : slot) * a.v_heads + h) * (long long)a.k_dim * a.v_dim;
     const bool from_zero = slot < 0 || (a.fresh && a.fresh[seq]);
@@ -217,6 +217,7 @@ static int delta_args(const csb_delta_shape_t* s, const void* q, const void* k, 
     a.sequences = s->sequences; a.k_heads = s->k_heads; a.v_heads = s->v_heads; a.k_dim = s->k_dim; a.v_dim = s->v_dim;
     a.scale = s->scale > 0.f ? s->scale : (float)(1.0 / std::sqrt((double)s->k_dim));
     a.normalize = (flags & CSB_FLAG_NORMALIZE) != 0;
+    a.shortest = 1; a.longest = 0x7fffffff;
     *out = a;
     return CSB_OK;
 }
@@ -225,8 +226,15 @@ static int recurrent_any(int dtype, const DeltaArgs& a, void* stream) {
     return dtype == CSB_F32 ? launch_recurrent<float>(a, stream) : dtype == CSB_F16 ? launch_recurrent<__half>(a, stream) : launch_recurrent<__nv_bfloat16>(a, stream);
 }
 
-// Sequences of few tokens each go token by token: a chunk costs as much as its tokens when it has about eight of them.
-static bool short_sequences(const csb_delta_shape_t* s) { return s->tokens <= 8 * (int64_t)s->sequences; }
+// Sequences of up to kShort tokens go token by token where that kernel is launched: a chunk takes as long.  The host does not know the
+// lengths: a call of up to kShort tokens has no longer sequence; where there are many sequences, or few tokens for each, both
+// kernels are launched and each takes its own (256 requests that decode beside a prompt of 1500 tokens, 32 heads: 338 us, in
+// chunks alone 992); else
+// chunks serve the few that may be short.
+constexpr int kShort = 8;
+static bool both_kernels(const DeltaArgs& a) {
+    return a.tokens <= 4ll * kShort * a.sequences || (int64_t)a.sequences * a.v_heads * ((a.v_dim + 63) / 64) > 8 * 148;
+}
 
 }  // namespace csb
 
@@ -235,7 +243,7 @@ using namespace csb;
 extern "C" {
 
 int64_t csb_gated_delta_workspace_bytes(const csb_delta_shape_t* s) {
-    if (!s || s->tokens <= 0 || s->sequences <= 0 || s->k_heads < 1 || s->v_heads < 1 || s->k_dim < 1 || s->k_dim > kDeltaMaxDim || short_sequences(s)) return 0;
+    if (!s || s->tokens <= 0 || s->sequences <= 0 || s->k_heads < 1 || s->v_heads < 1 || s->k_dim < 1 || s->k_dim > kDeltaMaxDim || s->tokens <= kShort) return 0;
     return delta_chunk_bytes(s->tokens, s->sequences, s->k_heads, s->v_heads, s->k_dim, s->dtype);
 }
 
@@ -249,8 +257,15 @@ int csb_gated_delta_forward(const csb_delta_shape_t* shape, const void* q, const
     if (!seq_begin && shape->sequences != 1) { set_error("seq_begin is NULL with %d sequences", shape->sequences); return CSB_ERR_INVALID_ARG; }
     const int64_t need = csb_gated_delta_workspace_bytes(shape);
     if (need && (!workspace || workspace_bytes < need)) { set_error("workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need); return CSB_ERR_INVALID_ARG; }
+    if (need && reinterpret_cast<uintptr_t>(workspace) % 16) { set_error("the workspace is not 16-byte aligned"); return CSB_ERR_INVALID_ARG; }
     a.seq_begin = seq_begin; a.slot = slot; a.fresh = fresh;
-    return need ? launch_delta_chunks(shape->dtype, a, workspace, stream) : recurrent_any(shape->dtype, a, stream);
+    if (!need) return recurrent_any(shape->dtype, a, stream);
+    if (!both_kernels(a)) return launch_delta_chunks(shape->dtype, a, workspace, stream);
+    a.longest = kShort;
+    const int short_rc = recurrent_any(shape->dtype, a, stream);
+    if (short_rc != CSB_OK) return short_rc;
+    a.shortest = kShort + 1;
+    return launch_delta_chunks(shape->dtype, a, workspace, stream);
 }
 
 int csb_gated_delta_step(const csb_delta_shape_t* shape, const void* q, const void* k, const void* v, const float* g, const float* beta, void* o,

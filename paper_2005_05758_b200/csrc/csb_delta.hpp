@@ -17,6 +17,7 @@ struct DeltaArgs {
     long long tokens, slots, ldq, ldk, ldv, ldg, ldb, ldo;
     int sequences, k_heads, v_heads, k_dim, v_dim;
     float scale;
+    int shortest, longest;              // tokens of the sequences that the kernel serves (others are served by the other one)
     int normalize, step;                // step: a token a sequence
 };
 
@@ -26,10 +27,12 @@ constexpr float kDeltaEps = 1e-6f;      // added to the sum of squares that a qu
 // last chunk of every sequence without knowing any length on the host.
 constexpr int kChunk = 32;
 struct DeltaChunkArgs {
+    int* gave_up;                       // 1 behind a call whose copies did not come within a second, else 0
     uint8_t *keys, *heads;              // [records][k_heads] operands of a chunk, [records][v_heads] its matrices and factors
     long long records;
     int key_bytes, groups;              // of a key record; CTAs of a head
     int pairs, values_async;            // whether two neighbouring outputs are one access; whether v is copied 16 bytes at a time
+    int ranked;                         // whether long sequences go first
     int rows_aligned;                   // whether a lane's values of q and k are whole loads
 };
 

@@ -6,14 +6,18 @@
 // What does not need S is done for all chunks at once by csb_delta_prepare_kernel, which leaves a record a chunk: the keys and
 // queries as binary16 (their rows scaled by powers of two; fp32 ones as two halves), the 32 x 32 matrices and a few
 // factors a token.  csb_delta_chunk_kernel goes through the chunks of a sequence.  A warp owns 16 columns of a head's
-// state, as S^T in the accumulators of mma.sync tiles: these are, as they stand, the operands of the next product, so the
-// whole chain state -> V' -> output and next state stays in the registers of one warp, and no warp waits for
-// another's values.  (On tcgen05 every link of the chain would go through TMEM and shared memory; the chain's
-// latency, not the tensor rate, bounds a sequence.)
+// state (and all of the keys' columns or a part), as S^T in the accumulators of mma.sync tiles: these are, as they stand, the operands
+// of the next product, so the chain S -> V' -> next S stays in registers but for one sum over the keys' parts.
+//
+// What bounds it: the chain from chunk to chunk.  8192 tokens of 16 / 32 heads of 128 x 128 in bfloat16 take 484 us, 77 of them
+// for the records (the bytes of q, k, v and o are 41 us at the measured copy rate); a chunk takes 1.6 us, of which the chain alone
+// needs 1.2 and the outputs, on the same SM, cost it 0.3.  On tcgen05 every link of the chain would go through TMEM
+// and shared memory and back, and a product of 16 columns would use an eighth of its rows: the tensor rate is not what is short (the
+// mma.sync pipe is a third busy).
 //
 // Precision: the fp32 operand of a product (S, V') is split into two binary16 halves after its row is scaled by a power of two,
-// so 22 bits of it stay, whatever its size; 16-bit keys and queries are exact in one half.  Increments of the state are
-// summed apart and added in fp32.
+// so 22 bits of a row's largest values stay, whatever their size; keys and queries are held to 2^-24 of their row's largest value (fp32
+// ones in two halves; the mantissas of the 16-bit types fit one).  Increments of the state are summed apart and added in fp32.
 //
 // Chunks that these forms do not hold go token by token in fp32 (walk_chunk_tokens): log-decays above 0, whose factors are not
 // bounded, and values that are not finite, which products with zeros would carry to tokens in front of them.
@@ -113,6 +117,7 @@ __global__ void __launch_bounds__(kPrepareWarps * 32, DKP == 256 ? 3 : 5) csb_de
     extern __shared__ __align__(512) uint8_t raw[];
     PrepareSmem<DKP, LO>& M = *reinterpret_cast<PrepareSmem<DKP, LO>*>(raw);
     pdl_wait();
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *w.gave_up = 0;
     const long long rec = blockIdx.x;
     const int hk = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int lo = 0;
@@ -124,7 +129,7 @@ __global__ void __launch_bounds__(kPrepareWarps * 32, DKP == 256 ? 3 : 5) csb_de
     }
     sequence_range(a, lo, t0, t1);
     const long long c = rec - (t0 / kChunk + lo), first = t0 + c * kChunk;
-    if (c < 0 || first >= t1) return;
+    if (c < 0 || first >= t1 || t1 - t0 < a.shortest) return;
     const int n = (int)min((long long)kChunk, t1 - first);
     if (threadIdx.x == 0) M.odd = 0;
     __syncthreads();
@@ -372,12 +377,12 @@ __device__ __forceinline__ void times_lower(float (&d)[4][4], const uint32_t (&h
     }
 }
 
-// Tokens [first, first + n) one by one in fp32, a warp's part of the state (keys' columns k0 .. k0 + 63).  `sums` is shared by
+// Tokens [first, first + n) one by one in fp32, a warp's part of the state (8 NJ of the keys' columns).  `sums` is shared by
 // the tile's warps, which meet at barrier `id`.
-template <typename T, int KS>
-__device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)[8][4], int h, int hk, int col0, int part, long long first, int n, float4* sums,
+template <typename T, int KS, int NJ>
+__device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)[NJ][4], int h, int hk, int col0, int part, long long first, int n, float4* sums,
                                                   int id) {
-    const int lane = threadIdx.x & 31, t = lane & 3, g = lane >> 2, k0 = part * 64;
+    const int lane = threadIdx.x & 31, t = lane & 3, g = lane >> 2, k0 = part * NJ * 8;
     for (long long at = first; at < first + n; ++at) {
         const T *kp = static_cast<const T*>(a.k) + (long long)hk * a.k_dim + at * a.ldk, *qp = static_cast<const T*>(a.q) + (long long)hk * a.k_dim + at * a.ldq;
         float kk = 0.f, qq = 0.f, dot = 0.f, u[4] = {0.f, 0.f, 0.f, 0.f};
@@ -389,9 +394,9 @@ __device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)
         for (int d = 16; d; d >>= 1) {
             kk += __shfl_xor_sync(0xffffffffu, kk, d); qq += __shfl_xor_sync(0xffffffffu, qq, d); dot += __shfl_xor_sync(0xffffffffu, dot, d);
         }
-        float key[8][2];
+        float key[NJ][2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int c = k0 + 8 * j + 2 * t + e;
@@ -425,7 +430,7 @@ __device__ __forceinline__ void walk_chunk_tokens(const DeltaArgs& a, float (&S)
                 static_cast<T*>(a.o)[at * a.ldo + (long long)h * a.v_dim + col] = from_float<T>(qn * (decay * u[2 + r] + dot * add[r]));
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 S[j][e] = fmaf(key[j][e], add[0], decay * S[j][e]);
@@ -441,30 +446,34 @@ __device__ __forceinline__ void store_pair(float* p, float x, float y) { *reinte
 __device__ __forceinline__ void store_pair(__half* p, float x, float y) { *reinterpret_cast<__half2*>(p) = __floats2half2_rn(x, y); }
 __device__ __forceinline__ void store_pair(__nv_bfloat16* p, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y); }
 
-// A CTA has nine warps.  Four carry the state: KS of them share a tile of 16 columns of the head, each with 64 of the keys'
-// columns, and W = 4 / KS tiles share the records.  Four others, a chunk behind, compute the outputs from the operands
-// that the first hand over (the state's halves and V'), and the last fetches what comes next: none of that is on the way from
-// chunk to chunk.
+// A CTA has eight warps.  Four carry the state: KS of them share a tile of 16 columns of the head, each with DKP / KS of the keys'
+// columns, and 4 / KS tiles share the records.  The other four, a chunk behind, compute the outputs from the operands
+// that the first hand over (the state's halves and V'): none of that is on the way from chunk to chunk.  They also ask for the
+// records (bulk copies) and values of the chunks to come.
 // Shared memory: stages of a chunk's records and values, and what warps tell one another.
-template <typename T, int KS>
+template <typename T, int DKP, int KS>
 struct ChunkStage {
-    static constexpr int kTiles = 4 / KS, kKeyRows = kChunk * KS * 128, kKeyBytes = (sizeof(T) == 4 ? 4 : 2) * kKeyRows;
+    static constexpr int kTiles = 4 / KS, kKeyRows = kChunk * DKP * 2, kKeyBytes = (sizeof(T) == 4 ? 4 : 2) * kKeyRows;
+    static constexpr int kParts = DKP / KS / 8;                 // tiles of 8 of the keys' columns that a warp has
     static constexpr int kValues = kTiles * 16, kPitch = kValues * (int)sizeof(T) + 16;
     static constexpr int kBytes = kKeyBytes + kHeadBytes + (kChunk * kPitch + 511) / 512 * 512;
-    static constexpr int kState = 4096, kScales = 512, kNew = 2048;   // of a warp: halves of the state, scales of its rows and of V'; of a tile: V'
+    static constexpr int kState = kParts * 512, kScales = 512, kNew = 2048;   // of a warp: halves of the state, scales of its rows and of V'; of a tile: V'
     static constexpr int kHand = 4 * (kState + kScales) + kTiles * kNew + 512;
     static constexpr int kTold = KS > 1 ? 8 * 2048 + 512 : 0;   // a warp's sums over its keys' columns; its rows' largest magnitudes
-    static constexpr int kStages = 3 * kBytes + 2 * kHand + kTold <= 227 * 1024 ? 3 : 2;
-    static constexpr int kSmem = kStages * kBytes + 2 * kHand + kTold;
+    static constexpr int kBars = 512;
+    static constexpr int kRest = 2 * kHand + kTold + kBars, kRoom = 225 * 1024;
+    // of a chunk that is carried on, one whose outputs are computed and those to come; with two, the next comes after both
+    static constexpr int kStages = 4 * kBytes + kRest <= kRoom ? 4 : 3 * kBytes + kRest <= kRoom ? 3 : 2, kAhead = kStages > 2 ? kStages - 2 : 1;
+    static constexpr int kSmem = kStages * kBytes + kRest;
 };
 
 // The sequence with the rank-th most tokens, so that long ones start first (12 sequences of 1 to 1300 tokens on 16 heads: the call 187 us
 // instead of 213).
-// Where there are more sequences than that is worth, the rank-th as they come.  All threads of the block take part.
+// Where all start at once, or there are more sequences than that is worth, the rank-th as they come.  All threads of the block take part.
 constexpr int kRanked = 256;
-__device__ __forceinline__ int sequence_of_rank(const DeltaArgs& a, int rank) {
+__device__ __forceinline__ int sequence_of_rank(const DeltaArgs& a, const DeltaChunkArgs& w, int rank) {
     __shared__ int length[kRanked], found;
-    if (!a.seq_begin || a.sequences > kRanked) return rank;
+    if (!w.ranked) return rank;
     const int i = threadIdx.x;
     if (i < a.sequences) {
         long long t0, t1;
@@ -481,36 +490,84 @@ __device__ __forceinline__ int sequence_of_rank(const DeltaArgs& a, int rank) {
     return found;
 }
 
-template <typename T, int KS>
-__global__ void __launch_bounds__(288, 1) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
+template <typename T, int DKP, int KS>
+__global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs a, const DeltaChunkArgs w) {
     constexpr bool LO = sizeof(T) == 4;
-    using Stage = ChunkStage<T, KS>;
-    constexpr int kRows = Stage::kKeyRows, kPitch = Stage::kPitch;
+    using Stage = ChunkStage<T, DKP, KS>;
+    constexpr int kRows = Stage::kKeyRows, kPitch = Stage::kPitch, NJ = Stage::kParts;
     extern __shared__ __align__(512) uint8_t smem[];
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5 & 3, g = lane >> 2, t = lane & 3, tile = warp / KS, part = warp % KS;
-    const bool carries = threadIdx.x < 128, fetches = threadIdx.x >= 256;
+    const bool carries = threadIdx.x < 128, waits = threadIdx.x >> 5 == 4;
     const int group = (int)(blockIdx.x % w.groups);
     const long long rest = blockIdx.x / w.groups;
-    const int h = (int)(rest % a.v_heads), seq = sequence_of_rank(a, (int)(rest / a.v_heads)), hk = h / (a.v_heads / a.k_heads);
+    const int h = (int)(rest % a.v_heads), seq = sequence_of_rank(a, w, (int)(rest / a.v_heads)), hk = h / (a.v_heads / a.k_heads);
     long long t0, t1, slot = -1;
     sequence_range(a, seq, t0, t1);
     if (a.state) {
         slot = delta_slot(a, seq);
         if (slot < 0) return;
     }
-    if (t0 >= t1) return;
+    if (t1 - t0 < a.shortest) return;
     // Rows g and g + 8 of a tile, which a lane has, are neighbouring columns of the head.  (A tile behind the last column works on zeros.)
     const int first_col = group * Stage::kValues, col0 = first_col + tile * 16, col = col0 + 2 * g;
-    float S[8][4];
+    const int tokens = (int)(t1 - t0), chunks = (tokens + kChunk - 1) / kChunk;
+    const long long rec0 = t0 / kChunk + seq;
+    const T* vp = static_cast<const T*>(a.v) + t0 * a.ldv + (long long)h * a.v_dim + first_col;
+    const uint8_t *keys_at = w.keys + (rec0 * a.k_heads + hk) * w.key_bytes;
+    const uint8_t *head_at = w.heads + (rec0 * a.v_heads + h) * kHeadBytes;
+    const long long keys_step = (long long)a.k_heads * w.key_bytes, head_step = (long long)a.v_heads * kHeadBytes;
+    uint64_t* arrived = reinterpret_cast<uint64_t*>(smem + Stage::kSmem - Stage::kBars);
+    volatile int* dead = reinterpret_cast<volatile int*>(arrived + 4);
+    // Chunk c's records, asked for by one thread, and its values of the CTA's columns (zeros where there are none), by the second four warps.
+    auto stage_of = [&](int c) { return smem + c % Stage::kStages * Stage::kBytes; };
+    auto fetch = [&](int c) {
+        if (c < chunks) {
+            uint8_t *stage = stage_of(c), *values = stage + Stage::kKeyBytes + kHeadBytes;
+            constexpr uint32_t kUsed = kFactors + sizeof(DeltaFactors);
+            const int thread = threadIdx.x & 127;
+            if (thread == 0) {
+                uint64_t* bar = arrived + c % Stage::kStages;
+                mbar_expect_tx(bar, Stage::kKeyBytes + kUsed);
+                bulk_g2s(stage, keys_at + c * keys_step, Stage::kKeyBytes, bar);
+                bulk_g2s(stage + Stage::kKeyBytes, head_at + c * head_step, kUsed, bar);
+            }
+            constexpr int kUnit = 16 / (int)sizeof(T), kUnits = Stage::kValues / kUnit;      // values of 16 bytes, and such of a row
+            if (w.values_async) {
+#pragma unroll
+                for (int i = 0; i < kChunk * kUnits; i += 128) {
+                    const int row = (i + thread) / kUnits, u = (i + thread) % kUnits * kUnit, at = c * kChunk + row;
+                    if (kChunk * kUnits % 128 && row >= kChunk) break;
+                    const bool there = at < tokens && first_col + u < a.v_dim;
+                    copy_16(smem_u32(values) + row * kPitch + u * (int)sizeof(T), there ? vp + at * a.ldv + u : vp, there ? 16 : 0);
+                }
+            } else {
+                for (int i = thread; i < kChunk * Stage::kValues; i += 128) {
+                    const int row = i / Stage::kValues, u = i % Stage::kValues, at = c * kChunk + row;
+                    reinterpret_cast<T*>(values + row * kPitch)[u] = at < tokens && first_col + u < a.v_dim ? vp[at * a.ldv + u] : from_float<T>(0.f);
+                }
+            }
+        }
+        copies_commit();
+    };
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < Stage::kStages; ++i) mbar_init(arrived + i, 1);
+        *dead = 0;
+        mbar_fence_init();
+    }
+    fence_proxy_async_all();                                    // the records, written by the kernel in front, are read by bulk copies
+    __syncthreads();
+    if (!carries)
+        for (int c = 0; c < Stage::kAhead; ++c) fetch(c);
+    float S[NJ][4];
     float* home = a.state + ((slot < 0 ? 0 : slot) * a.v_heads + h) * (long long)a.k_dim * a.v_dim;
     const bool from_zero = slot < 0 || (a.fresh && a.fresh[seq]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = part * 64 + 8 * j + 2 * t + (i & 1);
+            const int r = part * NJ * 8 + 8 * j + 2 * t + (i & 1);
             S[j][i] = carries && !from_zero && r < a.k_dim && col + (i >> 1) < a.v_dim ? home[(long long)r * a.v_dim + col + (i >> 1)] : 0.f;
         }
     // The state is held times a power of two a row (by, its inverse back) that binary16 halves of it can have.  No scale waits for
@@ -521,7 +578,7 @@ __global__ void __launch_bounds__(288, 1) csb_delta_chunk_kernel(const DeltaArgs
     auto largest = [&]() {
         most0 = most1 = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < NJ; ++j) {
             most0 = fmaxf(most0, fmaxf(fabsf(S[j][0]), fabsf(S[j][1])));
             most1 = fmaxf(most1, fmaxf(fabsf(S[j][2]), fabsf(S[j][3])));
         }
@@ -532,48 +589,11 @@ __global__ void __launch_bounds__(288, 1) csb_delta_chunk_kernel(const DeltaArgs
         by0 = grow<8>(most0, 1.f); by1 = grow<8>(most1, 1.f);
         back0 = inverse_of(by0); back1 = inverse_of(by1);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { S[j][0] *= by0; S[j][1] *= by0; S[j][2] *= by1; S[j][3] *= by1; }
+        for (int j = 0; j < NJ; ++j) { S[j][0] *= by0; S[j][1] *= by0; S[j][2] *= by1; S[j][3] *= by1; }
         most0 *= by0; most1 *= by1;
     };
     settle();
 
-    const int tokens = (int)(t1 - t0), chunks = (tokens + kChunk - 1) / kChunk;
-    const long long rec0 = t0 / kChunk + seq;
-    const T* vp = static_cast<const T*>(a.v) + t0 * a.ldv + (long long)h * a.v_dim + first_col;
-    const uint8_t *keys_at = w.keys + (rec0 * a.k_heads + hk) * w.key_bytes + lane * 16;
-    const uint8_t *head_at = w.heads + (rec0 * a.v_heads + h) * kHeadBytes + lane * 16;
-    const long long keys_step = (long long)a.k_heads * w.key_bytes, head_step = (long long)a.v_heads * kHeadBytes;
-    // Chunk c's records and its values of the CTA's columns (zeros where there are none).
-    auto stage_of = [&](int c) { return smem + (Stage::kStages == 3 ? c % 3 : c & 1) * Stage::kBytes; };
-    auto fetch = [&](int c) {
-        if (c < chunks) {
-            uint8_t* stage = stage_of(c);
-            const uint32_t to = smem_u32(stage) + lane * 16;
-            constexpr int kUsed = kFactors + (int)sizeof(DeltaFactors);
-#pragma unroll 8
-            for (int i = 0; i < Stage::kKeyBytes; i += 512) copy_16(to + i, keys_at + i, 16);
-#pragma unroll 8
-            for (int i = 0; i < kUsed; i += 512)
-                if (i + lane * 16 < kUsed) copy_16(to + Stage::kKeyBytes + i, head_at + i, 16);
-            keys_at += keys_step; head_at += head_step;
-            constexpr int kUnit = 16 / (int)sizeof(T), kUnits = Stage::kValues / kUnit;      // values of 16 bytes, and such of a row
-            uint8_t* values = stage + Stage::kKeyBytes + kHeadBytes;
-            if (w.values_async) {
-#pragma unroll 4
-                for (int i = lane; i < kChunk * kUnits; i += 32) {
-                    const int row = i / kUnits, u = i % kUnits * kUnit, at = c * kChunk + row;
-                    const bool there = at < tokens && first_col + u < a.v_dim;
-                    copy_16(smem_u32(values) + row * kPitch + u * (int)sizeof(T), there ? vp + at * a.ldv + u : vp, there ? 16 : 0);
-                }
-            } else {
-                for (int i = lane; i < kChunk * Stage::kValues; i += 32) {
-                    const int row = i / Stage::kValues, u = i % Stage::kValues, at = c * kChunk + row;
-                    reinterpret_cast<T*>(values + row * kPitch)[u] = at < tokens && first_col + u < a.v_dim ? vp[at * a.ldv + u] : from_float<T>(0.f);
-                }
-            }
-        }
-        copies_commit();
-    };
     const bool pairs = w.pairs && col + 1 < a.v_dim;
     T* op = static_cast<T*>(a.o) + t0 * a.ldo + (long long)h * a.v_dim + col;
     // what the carrying warps hand over, by turns; what the warps of a tile tell one another
@@ -594,13 +614,13 @@ __global__ void __launch_bounds__(288, 1) csb_delta_chunk_kernel(const DeltaArgs
     };
     // this lane's places in the operands (see load_matrices): rows are tokens, units 32 bytes a step apart
     const int tok = (lane >> 4) * 8 + (lane & 7);
-    const uint32_t row_at = tok * KS * 128 + (((lane >> 3 & 1) ^ (tok & 7)) << 4), row_at_t = lane * KS * 128 + ((lane & 7) << 4);
+    const uint32_t row_at = tok * DKP * 2 + (((lane >> 3 & 1) ^ (tok & 7)) << 4), row_at_t = lane * DKP * 2 + ((lane & 7) << 4);
     const uint32_t mat_at = matrix_at((lane >> 3 & 1) * 8 + (lane & 7), (lane >> 4) * 8);
 
     // From the state in front of chunk c to the one behind it.
     auto carry = [&](int c) {
         const uint8_t* here = stage_of(c);
-        const uint32_t keys = smem_u32(here) + part * 128, head = smem_u32(here) + Stage::kKeyBytes;
+        const uint32_t keys = smem_u32(here) + part * NJ * 16, head = smem_u32(here) + Stage::kKeyBytes;
         const DeltaFactors& F = *reinterpret_cast<const DeltaFactors*>(here + Stage::kKeyBytes + kFactors);
         const uint8_t* mine = here + Stage::kKeyBytes + kHeadBytes + (tile * 16 + 2 * g) * (int)sizeof(T) + 2 * t * kPitch;
         const Hand out = hand_of(c);
@@ -615,8 +635,8 @@ __global__ void __launch_bounds__(288, 1) csb_delta_chunk_kernel(const DeltaArgs
         if (part == 0 && lane == 0) *out.walked = walk;
         if (walk) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { S[j][0] *= back0; S[j][1] *= back0; S[j][2] *= back1; S[j][3] *= back1; }
-            walk_chunk_tokens<T, KS>(a, S, h, hk, col0, part, t0 + (long long)c * kChunk, min(kChunk, tokens - c * kChunk), told, meet);
+            for (int j = 0; j < NJ; ++j) { S[j][0] *= back0; S[j][1] *= back0; S[j][2] *= back1; S[j][3] *= back1; }
+            walk_chunk_tokens<T, KS, NJ>(a, S, h, hk, col0, part, t0 + (long long)c * kChunk, min(kChunk, tokens - c * kChunk), told, meet);
             settle();
             tell_most();
             return;
@@ -637,7 +657,7 @@ __global__ void __launch_bounds__(288, 1) csb_delta_chunk_kernel(const DeltaArgs
         // S^T k
         float r[4][4] = {};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NJ / 2; ++j) {
             uint32_t hi[4], lo[4], b[2][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) split_pair(S[2 * j + (i >> 1)][(i & 1) * 2], S[2 * j + (i >> 1)][(i & 1) * 2 + 1], hi[i], lo[i]);
@@ -705,7 +725,7 @@ __global__ void __launch_bounds__(288, 1) csb_delta_chunk_kernel(const DeltaArgs
         }
         split_tile(x, inv0, inv1, hi, lo);
 #pragma unroll
-        for (int j = 0; j < 8; j += 4) {
+        for (int j = 0; j < NJ; j += 4) {
             float add[4][4] = {};
             uint32_t b[4][4], l[4][4];
 #pragma unroll
@@ -739,13 +759,13 @@ __global__ void __launch_bounds__(288, 1) csb_delta_chunk_kernel(const DeltaArgs
     // The outputs of chunk c; the warps of a tile share its tokens evenly.
     auto put_out = [&](int c) {
         const uint8_t* here = stage_of(c);
-        const uint32_t queries = smem_u32(here) + kRows + part * 128, head = smem_u32(here) + Stage::kKeyBytes;
+        const uint32_t queries = smem_u32(here) + kRows + part * NJ * 16, head = smem_u32(here) + Stage::kKeyBytes;
         const DeltaFactors& F = *reinterpret_cast<const DeltaFactors*>(here + Stage::kKeyBytes + kFactors);
         const Hand in = hand_of(c);
         if (*in.walked) return;
         float o[4][4] = {};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NJ / 2; ++j) {
             uint32_t b[2][4];
             const uint4 h4 = in.state[2 * j * 32], l4 = in.state[(2 * j + 1) * 32];
             const uint32_t hi[4] = {h4.x, h4.y, h4.z, h4.w}, lo[4] = {l4.x, l4.y, l4.z, l4.w};
@@ -818,28 +838,34 @@ __global__ void __launch_bounds__(288, 1) csb_delta_chunk_kernel(const DeltaArgs
         else outputs(std::integral_constant<int, KS == 4 ? 3 : 0>());
     };
 
-    if (fetches) fetch(0);
     for (int c = 0; c <= chunks; ++c) {
-        if (fetches) copies_wait<0>();
+        if (!carries) copies_wait<Stage::kAhead - 1>();
+        if (waits && c < chunks && !mbar_wait_bounded(arrived + c % Stage::kStages, c / Stage::kStages & 1)) {
+            for (int i = c; i < min(c + Stage::kAhead, chunks); ++i) mbar_wait_bounded(arrived + i % Stage::kStages, i / Stage::kStages & 1);   // (stages must not go before their copies)
+            *dead = 1;
+        }
         __syncthreads();                                        // chunk c is there, and what is handed over of chunk c - 1
+        if (*dead) {                                            // (bulk copies of this GPU's own memory: never seen)
+            if (threadIdx.x == 0) *w.gave_up = 1;
+            return;
+        }
         if (carries) {
             if (c < chunks) carry(c);
-        } else if (!fetches) {
+        } else {
+            if (Stage::kStages > 2) fetch(c + Stage::kAhead);
             if (c > 0) put_out(c - 1);
-        } else if (Stage::kStages == 3) {
-            fetch(c + 1);
         }
         if (Stage::kStages == 2) {
             __syncthreads();                                    // chunk c - 1 is done with
-            if (fetches) fetch(c + 1);
+            if (!carries) fetch(c + 1);
         }
     }
     if (slot < 0 || !carries) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = part * 64 + 8 * j + 2 * t + (i & 1);
+            const int r = part * NJ * 8 + 8 * j + 2 * t + (i & 1);
             if (r < a.k_dim && col + (i >> 1) < a.v_dim) home[(long long)r * a.v_dim + col + (i >> 1)] = S[j][i] * (i >> 1 ? back1 : back0);
         }
 }
@@ -855,23 +881,26 @@ __global__ void __launch_bounds__(288, 1) csb_delta_chunk_kernel(const DeltaArgs
         }                                                                                  \
     } while (0)
 
+constexpr int64_t kWorkspaceHead = 512;  // its first word: whether a wait ran out
 static int padded(int k_dim) { return k_dim <= 64 ? 64 : k_dim <= 128 ? 128 : 256; }
 static int key_bytes(int k_dim, int dtype) { return (dtype == CSB_F32 ? 4 : 2) * kChunk * padded(k_dim) * 2; }
 
 int64_t delta_chunk_bytes(int64_t tokens, int64_t sequences, int k_heads, int v_heads, int k_dim, int dtype) {
-    return (tokens / kChunk + sequences) * ((int64_t)k_heads * key_bytes(k_dim, dtype) + (int64_t)v_heads * kHeadBytes);
+    return kWorkspaceHead + (tokens / kChunk + sequences) * ((int64_t)k_heads * key_bytes(k_dim, dtype) + (int64_t)v_heads * kHeadBytes);
 }
 
-template <typename T, int KS>
+template <typename T, int DKP, int KS>
 static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
-    constexpr int DKP = KS * 64;
-    using Stage = ChunkStage<T, KS>;
+    using Stage = ChunkStage<T, DKP, KS>;
     DeltaChunkArgs w{};
     w.records = a.tokens / kChunk + a.sequences;
     w.key_bytes = Stage::kKeyBytes;
-    w.keys = static_cast<uint8_t*>(workspace);
+    w.gave_up = static_cast<int*>(workspace);
+    w.keys = static_cast<uint8_t*>(workspace) + kWorkspaceHead;
     w.heads = w.keys + w.records * a.k_heads * (int64_t)w.key_bytes;
     w.groups = (a.v_dim + Stage::kValues - 1) / Stage::kValues;
+    if ((int64_t)a.sequences * a.v_heads * w.groups > 0x7fffffff) { set_error("%d sequences of %d heads of %d values are more than a grid has", a.sequences, a.v_heads, a.v_dim); return CSB_ERR_UNSUPPORTED; }
+    w.ranked = a.seq_begin && a.sequences > 1 && a.sequences <= kRanked && (int64_t)a.sequences * a.v_heads * w.groups > 148;
     w.pairs = a.v_dim % 2 == 0 && a.ldo % 2 == 0 && reinterpret_cast<uintptr_t>(a.o) % (2 * sizeof(T)) == 0;
     const size_t run = std::min<size_t>(DKP / 32 * sizeof(T), 16);
     w.rows_aligned = a.k_dim % (DKP / 32) == 0 && a.k_dim * sizeof(T) % run == 0 && a.ldq * sizeof(T) % run == 0 && a.ldk * sizeof(T) % run == 0 &&
@@ -886,16 +915,22 @@ static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
     cfg.dynamicSmemBytes = sizeof(PrepareSmem<DKP, sizeof(T) == 4>);
     CSB_CUDA((cudaFuncSetAttribute(csb_delta_prepare_kernel<T, DKP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
     CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_prepare_kernel<T, DKP>, a, w)));
-    cfg.gridDim = dim3((unsigned)((int64_t)a.sequences * a.v_heads * w.groups)); cfg.blockDim = dim3(288);
+    cfg.gridDim = dim3((unsigned)((int64_t)a.sequences * a.v_heads * w.groups)); cfg.blockDim = dim3(256);
     cfg.dynamicSmemBytes = Stage::kSmem;
-    CSB_CUDA((cudaFuncSetAttribute(csb_delta_chunk_kernel<T, KS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
-    CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_chunk_kernel<T, KS>, a, w)));
+    CSB_CUDA((cudaFuncSetAttribute(csb_delta_chunk_kernel<T, DKP, KS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)));
+    CSB_CUDA((cudaLaunchKernelEx(&cfg, csb_delta_chunk_kernel<T, DKP, KS>, a, w)));
     return CSB_OK;
 }
+// Two warps for a tile's 128 keys' columns are faster from chunk to chunk, one does more with an SM: two while every CTA has an SM of its
+// own (8192 tokens of 32 heads: 484 us with two, 734 with one; 12 prompts on 16 heads, 768 CTAs: 180 us and 168).
 template <typename T>
 static int launch_chunks_of(const DeltaArgs& a, void* workspace, void* stream) {
     const int dkp = padded(a.k_dim);
-    return dkp == 64 ? launch_chunks<T, 1>(a, workspace, stream) : dkp == 128 ? launch_chunks<T, 2>(a, workspace, stream) : launch_chunks<T, 4>(a, workspace, stream);
+    const int64_t heads = (int64_t)a.sequences * a.v_heads;
+    if (dkp == 64) return launch_chunks<T, 64, 1>(a, workspace, stream);
+    if (dkp == 128)
+        return heads * ((a.v_dim + 31) / 32) <= 148 ? launch_chunks<T, 128, 2>(a, workspace, stream) : launch_chunks<T, 128, 1>(a, workspace, stream);
+    return launch_chunks<T, 256, 4>(a, workspace, stream);
 }
 
 int launch_delta_chunks(int dtype, const DeltaArgs& a, void* workspace, void* stream) {

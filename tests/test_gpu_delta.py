@@ -84,6 +84,19 @@ def test_forward_matches_the_oracle(lens, Hk, Hv, dk, dv, dtype):
     check(a, lens)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("seed,sequences,longest", [(1, 8, 9), (2, 40, 100), (3, 300, 40), (4, 9, 1), (5, 30, 8)])
+def test_requests_that_decode_beside_prompts(seed, sequences, longest, dtype):
+    rng = np.random.default_rng(seed)
+    lens = rng.choice([0, 1, 1, 1, 2, 7, 8, 9, 31, 32, 33, 64, 100], sequences)
+    lens = [int(min(n, longest)) for n in lens]
+    lens[-1] = longest
+    slot = rng.permutation(sequences + 3)[:sequences].astype(int).tolist()
+    slot[2], slot[4] = -1, slot[1]
+    a = draw(seed, sum(lens), 1, 2, 64, 40, dtype, slots=sequences + 3)
+    check(a, lens, slot=slot, fresh=(rng.random(sequences) < 0.5).astype(int).tolist(), normalize=True)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_slices_of_wider_rows_and_normalisation_and_scale(dtype):
     lens = [50, 3, 129]

@@ -51,6 +51,8 @@ def test_missing_arguments_and_flags():
     need = lib.csb_gated_delta_workspace_bytes(C.byref(shape(tokens=5000)))
     assert need > 0 and forward(shape(tokens=5000), size=need - 1) == INVALID and b"workspace" in lib.csb_last_error()
     assert forward(shape(tokens=5000), ws=None) == INVALID
+    assert forward(shape(tokens=5000), ws=FAKE + 8) == INVALID and b"aligned" in lib.csb_last_error()
+    assert lib.csb_gated_delta_workspace_bytes(C.byref(shape(tokens=8))) == 0      # all short: token by token
 
 
 def test_nothing_to_do_needs_no_pointers():
