@@ -437,6 +437,7 @@ int csb_spmm_adapters(const csb_matrix_t* A, const float* X, int64_t ldx, int ba
     if (ldx < A->cols || ldy < A->rows) { set_error("ldx=%lld < cols or ldy=%lld < rows", (long long)ldx, (long long)ldy); return CSB_ERR_SHAPE; }
     const int64_t need = csb::workspace_bytes(A->cols, batch, rank);
     if (count > 0 && workspace_size < need) { set_error("workspace of %lld bytes, %lld needed", (long long)workspace_size, (long long)need); return CSB_ERR_INVALID_ARG; }
+    if (count > 0 && reinterpret_cast<uintptr_t>(workspace) % 4) { set_error("the workspace is not 4-byte aligned"); return CSB_ERR_INVALID_ARG; }
     if (A->device < 0) { set_error("matrix was encoded host-only (device = -1)"); return CSB_ERR_UNSUPPORTED; }
     if (A->val_dtype == CSB_Q16) { set_error("fixed-point handles serve csb_spmm_q16 only"); return CSB_ERR_UNSUPPORTED; }
     int current = -1;

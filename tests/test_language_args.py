@@ -76,7 +76,7 @@ def test_adapters_that_are_refused():
     A = host_matrix()
     assert adapters(None) == INVALID
     for changed in (dict(batch=-1), dict(count=-1), dict(rank=0), dict(X=None), dict(Y=None), dict(which=None), dict(down=None), dict(up=None), dict(ws=None),
-                    dict(size=1)):
+                    dict(size=1), dict(ws=FAKE + 2)):
         assert adapters(A, **changed) == INVALID, changed
     assert adapters(A, dtype=2) == DTYPE and adapters(A, dtype=-1) == DTYPE
     assert adapters(A, ldx=11) == SHAPE and adapters(A, ldy=7) == SHAPE
