@@ -231,7 +231,7 @@ static int recurrent_any(int dtype, const DeltaArgs& a, void* stream) {
 // kernels are launched and each takes its own (256 requests that decode beside a prompt of 1500 tokens, 32 heads: 338 us, in
 // chunks alone 992); else
 // chunks serve the few that may be short.
-constexpr int kShort = 8;
+constexpr int kShort = kLong - 1;
 static bool both_kernels(const DeltaArgs& a) {
     return a.tokens <= 4ll * kShort * a.sequences || (int64_t)a.sequences * a.v_heads * ((a.v_dim + 63) / 64) > 8 * 148;
 }

@@ -23,13 +23,15 @@ struct DeltaArgs {
 
 constexpr float kDeltaEps = 1e-6f;      // added to the sum of squares that a query or key is divided by the root of
 
-// Chunks of tokens (csb_delta_chunk.cu).  Chunk c of sequence i has record begin_i / kChunk + i + c, which leaves room for the
-// last chunk of every sequence without knowing any length on the host.
+// Chunks of tokens (csb_delta_chunk.cu).  Chunk c of sequence i, whose first token is t, has a record that depends on no length:
+// t / kChunk + i + c of tokens / kChunk + sequences; or, where there are more sequences than the call can have long ones (those of
+// fewer than kLong tokens have no chunks then), t / kLong for the first chunk, and behind those t / kChunk + c for the others.
+constexpr int kLong = 9;
 constexpr int kChunk = 32;
 struct DeltaChunkArgs {
     int* gave_up;                       // 1 behind a call whose copies did not come within a second, else 0
     uint8_t *keys, *heads;              // [records][k_heads] operands of a chunk, [records][v_heads] its matrices and factors
-    long long records;
+    long long records, firsts;          // in all; in the second way for first chunks (0: the first way)
     int key_bytes, groups;              // of a key record; CTAs of a head
     int pairs, values_async;            // whether two neighbouring outputs are one access; whether v is copied 16 bytes at a time
     int ranked;                         // whether long sequences go first

@@ -120,16 +120,19 @@ __global__ void __launch_bounds__(kPrepareWarps * 32, DKP == 256 ? 3 : 5) csb_de
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *w.gave_up = 0;
     const long long rec = blockIdx.x;
     const int hk = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // the last sequence whose first record is not behind this one (in the second way: that starts early enough to have it)
+    const long long before = rec < w.firsts ? rec * kLong + kLong - 1 : (rec - w.firsts) * kChunk - 1;
     int lo = 0;
     long long t0, t1;
-    for (int hi = a.sequences; hi - lo > 1;) {           // the last sequence whose first record is not behind this one
+    for (int hi = a.sequences; hi - lo > 1;) {
         const int mid = lo + (hi - lo) / 2;
         sequence_range(a, mid, t0, t1);
-        if (t0 / kChunk + mid <= rec) lo = mid; else hi = mid;
+        if (w.firsts ? t0 <= before : t0 / kChunk + mid <= rec) lo = mid; else hi = mid;
     }
     sequence_range(a, lo, t0, t1);
-    const long long c = rec - (t0 / kChunk + lo), first = t0 + c * kChunk;
-    if (c < 0 || first >= t1 || t1 - t0 < a.shortest) return;
+    const long long c = !w.firsts ? rec - (t0 / kChunk + lo) : rec >= w.firsts ? rec - w.firsts - t0 / kChunk : t0 / kLong == rec ? 0 : -1;
+    const long long first = t0 + c * kChunk;
+    if (c < 0 || (c == 0 && rec >= w.firsts && w.firsts) || first >= t1 || t1 - t0 < a.shortest) return;
     const int n = (int)min((long long)kChunk, t1 - first);
     if (threadIdx.x == 0) M.odd = 0;
     __syncthreads();
@@ -513,11 +516,9 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
     // Rows g and g + 8 of a tile, which a lane has, are neighbouring columns of the head.  (A tile behind the last column works on zeros.)
     const int first_col = group * Stage::kValues, col0 = first_col + tile * 16, col = col0 + 2 * g;
     const int tokens = (int)(t1 - t0), chunks = (tokens + kChunk - 1) / kChunk;
-    const long long rec0 = t0 / kChunk + seq;
+    const long long rec0 = t0 / kChunk + (w.firsts ? w.firsts : seq);          // of chunk c, less c; the first one's may be another
+    const long long rec_first = w.firsts ? t0 / kLong : rec0;
     const T* vp = static_cast<const T*>(a.v) + t0 * a.ldv + (long long)h * a.v_dim + first_col;
-    const uint8_t *keys_at = w.keys + (rec0 * a.k_heads + hk) * w.key_bytes;
-    const uint8_t *head_at = w.heads + (rec0 * a.v_heads + h) * kHeadBytes;
-    const long long keys_step = (long long)a.k_heads * w.key_bytes, head_step = (long long)a.v_heads * kHeadBytes;
     uint64_t* arrived = reinterpret_cast<uint64_t*>(smem + Stage::kSmem - Stage::kBars);
     volatile int* dead = reinterpret_cast<volatile int*>(arrived + 4);
     // Chunk c's records, asked for by one thread, and its values of the CTA's columns (zeros where there are none), by the second four warps.
@@ -530,8 +531,9 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
             if (thread == 0) {
                 uint64_t* bar = arrived + c % Stage::kStages;
                 mbar_expect_tx(bar, Stage::kKeyBytes + kUsed);
-                bulk_g2s(stage, keys_at + c * keys_step, Stage::kKeyBytes, bar);
-                bulk_g2s(stage + Stage::kKeyBytes, head_at + c * head_step, kUsed, bar);
+                const long long rec = c ? rec0 + c : rec_first;
+                bulk_g2s(stage, w.keys + (rec * a.k_heads + hk) * w.key_bytes, Stage::kKeyBytes, bar);
+                bulk_g2s(stage + Stage::kKeyBytes, w.heads + (rec * a.v_heads + h) * kHeadBytes, kUsed, bar);
             }
             constexpr int kUnit = 16 / (int)sizeof(T), kUnits = Stage::kValues / kUnit;      // values of 16 bytes, and such of a row
             if (w.values_async) {
@@ -885,15 +887,25 @@ constexpr int64_t kWorkspaceHead = 512;  // its first word: whether a wait ran o
 static int padded(int k_dim) { return k_dim <= 64 ? 64 : k_dim <= 128 ? 128 : 256; }
 static int key_bytes(int k_dim, int dtype) { return (dtype == CSB_F32 ? 4 : 2) * kChunk * padded(k_dim) * 2; }
 
+// First chunks that a call of so many sequences can have where only those of kLong tokens or more have chunks; 0 where there are no
+// fewer of them than sequences.
+static int64_t first_records(int64_t tokens, int64_t sequences) { return sequences > tokens / kLong + 1 ? tokens / kLong + 1 : 0; }
+static int64_t all_records(int64_t tokens, int64_t sequences) {
+    const int64_t firsts = first_records(tokens, sequences);
+    return tokens / kChunk + (firsts ? firsts + 1 : sequences);
+}
+
 int64_t delta_chunk_bytes(int64_t tokens, int64_t sequences, int k_heads, int v_heads, int k_dim, int dtype) {
-    return kWorkspaceHead + (tokens / kChunk + sequences) * ((int64_t)k_heads * key_bytes(k_dim, dtype) + (int64_t)v_heads * kHeadBytes);
+    return kWorkspaceHead + all_records(tokens, sequences) * ((int64_t)k_heads * key_bytes(k_dim, dtype) + (int64_t)v_heads * kHeadBytes);
 }
 
 template <typename T, int DKP, int KS>
 static int launch_chunks(const DeltaArgs& a, void* workspace, void* stream) {
     using Stage = ChunkStage<T, DKP, KS>;
     DeltaChunkArgs w{};
-    w.records = a.tokens / kChunk + a.sequences;
+    w.records = all_records(a.tokens, a.sequences);
+    w.firsts = first_records(a.tokens, a.sequences);
+    if (w.firsts && a.shortest < kLong) { set_error("chunks of %d sequences of %lld tokens", a.sequences, a.tokens); return CSB_ERR_UNSUPPORTED; }   // (the caller serves short ones then)
     w.key_bytes = Stage::kKeyBytes;
     w.gave_up = static_cast<int*>(workspace);
     w.keys = static_cast<uint8_t*>(workspace) + kWorkspaceHead;

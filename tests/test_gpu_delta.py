@@ -97,6 +97,14 @@ def test_requests_that_decode_beside_prompts(seed, sequences, longest, dtype):
     check(a, lens, slot=slot, fresh=(rng.random(sequences) < 0.5).astype(int).tolist(), normalize=True)
 
 
+@pytest.mark.parametrize("lens", [[1] * 200 + [40] + [1] * 100 + [9, 0, 8, 70, 9, 33, 9] + [1] * 60, [33] + [0] * 30 + [9, 9], [2] * 50 + [64], [1] * 12 + [32, 31]])
+def test_few_prompts_among_many_tokens(lens):
+    a = draw(len(lens), sum(lens), 2, 2, 64, 32, "f16", slots=len(lens))
+    check(a, lens)
+    need = binding.lib.csb_gated_delta_workspace_bytes(binding.csb_delta_shape_t(1000, 1000, 1000, 16, 32, 128, 128, binding.CSB_BF16, 2048, 2048, 4096, 32, 32, 4096, 0.0))
+    assert need < 100 << 20                                      # no record for every sequence
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_slices_of_wider_rows_and_normalisation_and_scale(dtype):
     lens = [50, 3, 129]
