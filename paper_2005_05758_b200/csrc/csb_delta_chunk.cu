@@ -462,7 +462,7 @@ struct ChunkStage {
     static constexpr int kBytes = kKeyBytes + kHeadBytes + (kChunk * kPitch + 511) / 512 * 512;
     static constexpr int kState = kParts * 512, kScales = 512, kNew = 2048;   // of a warp: halves of the state, scales of its rows and of V'; of a tile: V'
     static constexpr int kHand = 4 * (kState + kScales) + kTiles * kNew + 512;
-    static constexpr int kTold = KS > 1 ? 8 * 2048 + 512 : 0;   // a warp's sums over its keys' columns; its rows' largest magnitudes
+    static constexpr int kTold = KS > 1 ? 4 * 2048 + 512 : 0;   // a warp's sums over its keys' columns; its rows' largest magnitudes
     static constexpr int kBars = 512;
     static constexpr int kRest = 2 * kHand + kTold + kBars, kRoom = 225 * 1024;
     // of a chunk that is carried on, one whose outputs are computed and those to come; with two, the next comes after both
@@ -600,9 +600,9 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
     T* op = static_cast<T*>(a.o) + t0 * a.ldo + (long long)h * a.v_dim + col;
     // what the carrying warps hand over, by turns; what the warps of a tile tell one another
     uint8_t* hands = smem + Stage::kStages * Stage::kBytes;
-    float4* told = reinterpret_cast<float4*>(hands + 2 * Stage::kHand + ((carries ? 0 : 4) + tile * KS) * 2048);
-    const int meet = (carries ? 1 : 5) + tile;
-    float2* mosts = reinterpret_cast<float2*>(hands + 2 * Stage::kHand + 8 * 2048) + tile * KS * 8 + g;
+    float4* told = reinterpret_cast<float4*>(hands + 2 * Stage::kHand + tile * KS * 2048);
+    const int meet = 1 + tile;
+    float2* mosts = reinterpret_cast<float2*>(hands + 2 * Stage::kHand + 4 * 2048) + tile * KS * 8 + g;
     auto tell_most = [&]() {                                     // (true magnitudes; read by the tile's warps in the next chunk)
         if (KS > 1 && t == 0) mosts[part * 8] = make_float2(most0 * back0, most1 * back1);
     };
@@ -688,10 +688,15 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
             tile_barrier<KS>(meet);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float4 f = told[i * 32 + lane];
+                if (KS == 2) {                                  // (two sum to the same in either order)
+                    const float4 f = told[(1 - part) * 128 + i * 32 + lane];
+                    r[i][0] += f.x; r[i][1] += f.y; r[i][2] += f.z; r[i][3] += f.w;
+                } else {
+                    float4 f = told[i * 32 + lane];
 #pragma unroll
-                for (int p = 1; p < KS; ++p) { const float4 e = told[p * 128 + i * 32 + lane]; f.x += e.x; f.y += e.y; f.z += e.z; f.w += e.w; }
-                r[i][0] = f.x; r[i][1] = f.y; r[i][2] = f.z; r[i][3] = f.w;
+                    for (int p = 1; p < KS; ++p) { const float4 e = told[p * 128 + i * 32 + lane]; f.x += e.x; f.y += e.y; f.z += e.z; f.w += e.w; }
+                    r[i][0] = f.x; r[i][1] = f.y; r[i][2] = f.z; r[i][3] = f.w;
+                }
             }
         }
         // what the tokens bring, less what the state holds for their keys
@@ -761,38 +766,10 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
     // The outputs of chunk c; the warps of a tile share its tokens evenly.
     auto put_out = [&](int c) {
         const uint8_t* here = stage_of(c);
-        const uint32_t queries = smem_u32(here) + kRows + part * NJ * 16, head = smem_u32(here) + Stage::kKeyBytes;
+        const uint32_t queries = smem_u32(here) + kRows, head = smem_u32(here) + Stage::kKeyBytes;
         const DeltaFactors& F = *reinterpret_cast<const DeltaFactors*>(here + Stage::kKeyBytes + kFactors);
         const Hand in = hand_of(c);
         if (*in.walked) return;
-        float o[4][4] = {};
-#pragma unroll
-        for (int j = 0; j < NJ / 2; ++j) {
-            uint32_t b[2][4];
-            const uint4 h4 = in.state[2 * j * 32], l4 = in.state[(2 * j + 1) * 32];
-            const uint32_t hi[4] = {h4.x, h4.y, h4.z, h4.w}, lo[4] = {l4.x, l4.y, l4.z, l4.w};
-            const uint32_t at = queries + (row_at ^ (32 * j));
-            load_matrices(b[0], at);
-            load_matrices(b[1], at + kRows / 2);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mma_f16(o[i], lo, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mma_f16(o[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
-            if (LO) {
-                load_matrices(b[0], at + 2 * kRows);
-                load_matrices(b[1], at + 2 * kRows + kRows / 2);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mma_f16(o[i], hi, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
-            }
-        }
-        const float4 back = *in.scales;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { o[i][0] *= back.x; o[i][1] *= back.x; o[i][2] *= back.y; o[i][3] *= back.y; }
-        if (KS > 1) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) told[part * 128 + i * 32 + lane] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
-            tile_barrier<KS>(meet);
-        }
         float x[4][4], inv0, inv1;
         uint32_t hi[2][4], lo[2][4];
 #pragma unroll
@@ -800,28 +777,55 @@ __global__ void __launch_bounds__(256, 1) csb_delta_chunk_kernel(const DeltaArgs
             const float4 f = in.fresh[i * 32];
             x[i][0] = f.x; x[i][1] = f.y; x[i][2] = f.z; x[i][3] = f.w;
         }
-        {
-            const float s0 = scale_of<13>(back.z, inv0), s1 = scale_of<13>(back.w, inv1);
-            split_tile(x, s0, s1, hi, lo);
-        }
         constexpr int kMine = 4 / KS;
         auto outputs = [&](auto from) {
             constexpr int FROM = decltype(from)::value;
+            // S^T q of the warp's tokens, from the halves of all parts of the state
+            float o[4][4] = {};
+            float4 back;
+#pragma unroll
+            for (int p = 0; p < KS; ++p) {
+                float d[4][4] = {};
+                const uint4* state = in.state + (p - part) * (Stage::kState / 16);
+                back = in.scales[(p - part) * (Stage::kScales / 16)];
+#pragma unroll
+                for (int j = 0; j < NJ / 2; ++j) {
+                    uint32_t b[2][4];
+                    const uint4 h4 = state[2 * j * 32], l4 = state[(2 * j + 1) * 32];
+                    const uint32_t sh[4] = {h4.x, h4.y, h4.z, h4.w}, sl[4] = {l4.x, l4.y, l4.z, l4.w};
+                    const uint32_t at = queries + p * NJ * 16 + (row_at ^ (32 * j));
+#pragma unroll
+                    for (int i = FROM / 2; 2 * i < FROM + kMine; ++i) load_matrices(b[i], at + i * (kRows / 2));
+#pragma unroll
+                    for (int i = FROM; i < FROM + kMine; ++i) mma_f16(d[i], sl, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+#pragma unroll
+                    for (int i = FROM; i < FROM + kMine; ++i) mma_f16(d[i], sh, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+                    if (LO) {
+#pragma unroll
+                        for (int i = FROM / 2; 2 * i < FROM + kMine; ++i) load_matrices(b[i], at + 2 * kRows + i * (kRows / 2));
+#pragma unroll
+                        for (int i = FROM; i < FROM + kMine; ++i) mma_f16(d[i], sh, b[i >> 1][(i & 1) * 2], b[i >> 1][(i & 1) * 2 + 1]);
+                    }
+                }
+#pragma unroll
+                for (int i = FROM; i < FROM + kMine; ++i) {
+                    o[i][0] = fmaf(d[i][0], back.x, o[i][0]); o[i][1] = fmaf(d[i][1], back.x, o[i][1]);
+                    o[i][2] = fmaf(d[i][2], back.y, o[i][2]); o[i][3] = fmaf(d[i][3], back.y, o[i][3]);
+                }
+            }
+            {
+                const float s0 = scale_of<13>(back.z, inv0), s1 = scale_of<13>(back.w, inv1);      // (the same for all parts)
+                split_tile(x, s0, s1, hi, lo);
+            }
             float inner[4][4] = {};
             times_lower<FROM, FROM + kMine>(inner, hi, lo, head + kInnerHi + mat_at, kInnerLo - kInnerHi);
 #pragma unroll
             for (int i = FROM; i < FROM + kMine; ++i) {
-                float4 f = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
-                if (KS > 1) {
-                    f = told[i * 32 + lane];
-#pragma unroll
-                    for (int p = 1; p < KS; ++p) { const float4 e = told[p * 128 + i * 32 + lane]; f.x += e.x; f.y += e.y; f.z += e.z; f.w += e.w; }
-                }
                 const float2 fs = *reinterpret_cast<const float2*>(&F.from_state[8 * i + 2 * t]), fc = *reinterpret_cast<const float2*>(&F.from_chunk[8 * i + 2 * t]);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const float ci = k ? fc.y : fc.x, cs = k ? fs.y : fs.x;
-                    const float x0 = fmaf(inner[i][k], ci * inv0, cs * (k ? f.y : f.x)), x1 = fmaf(inner[i][2 + k], ci * inv1, cs * (k ? f.w : f.z));
+                    const float x0 = fmaf(inner[i][k], ci * inv0, cs * o[i][k]), x1 = fmaf(inner[i][2 + k], ci * inv1, cs * o[i][2 + k]);
                     const int at = c * kChunk + 8 * i + 2 * t + k;
                     T* p = op + at * a.ldo;
                     if (at < tokens) {
