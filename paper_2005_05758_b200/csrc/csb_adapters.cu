@@ -1,9 +1,10 @@
 // The batched product with a low-rank adapter of its own for every request beside the shared matrix:
 //   Y[b, :] = W X[b, :] + s_a up_a (down_a X[b, :]),  a = which[b].
 // The shared product is csb_spmm's.  The adapters' part is two kernels around it: csb_adapter_down_kernel takes
-// down_a X[b, :] into the workspace, csb_adapter_up_kernel adds up_a times that to Y.  Requests of one adapter are taken
+// down_a X[b, :] into the workspace, csb_adapter_up_kernel adds up_a times that to Y; or, where there are few ranks and columns, one
+// behind it, csb_adapter_kernel.  Requests of one adapter are taken
 // eight at a time (the eight columns of a tensor-core tile), found by every CTA for itself from `which`: nothing is sorted
-// beforehand and no order of atomics enters.  Both kernels are bound by reading the adapters once; the arithmetic is in two tf32
+// beforehand and no order of atomics enters.  The kernels are bound by reading the adapters once; the arithmetic is in two tf32
 // halves of the fp32 operand (22 bits; 16-bit adapters are one such half exactly, fp32 adapters two), fp32 sums.
 #include <algorithm>
 
@@ -176,31 +177,19 @@ __device__ __forceinline__ void eight(const T* row, int c, int size, bool there,
     }
 }
 
-// part[split][b][:] = down_a X[b, columns of the split].  A warp takes 32 columns at a time: lane 4g + t has columns
-// 8t .. 8t + 7 of ranks g and g + 8 and of request g, which are its operands of four steps of eight columns when those are
-// counted in another order, so that every operand comes by wide loads straight from global memory.
+// sum[warp][request][rank] = down_a X[request, the warp's columns of c_begin .. c_end - 1], MT times 16 ranks from r0 on.  A warp takes 32
+// columns at a time: lane 4g + t has columns 8t .. 8t + 7 of ranks g and g + 8 and of request g, which are its operands of four steps
+// of eight columns when those are counted in another order, so that every operand comes by wide loads straight from global memory.
 template <typename T, int MT, bool VEC>
-__global__ void __launch_bounds__(kDownThreads) csb_adapter_down_kernel(AdapterArgs a) {
-    __shared__ Group G;
-    __shared__ float sum[kDownThreads / 32][MT * 16 * kGroup];
-    pdl_launch_dependents();
-    pdl_wait();
-    const int n = find_group<kDownThreads>(a, blockIdx.x, G);
-    if (blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < 2 + kGroup) {
-        const int i = threadIdx.x;
-        a.groups[blockIdx.x * kGroupWords + i] = i == 0 ? (n ? G.adapter : 0) : i == 1 ? n : i - 2 < n ? G.member[i - 2] : 0;
-    }
-    if (!n) return;
-    const int which = G.adapter, rank = rank_of(a, which), r0 = (int)blockIdx.z * MT * 16;
-    if (r0 >= rank) return;                                      // (the other kernel reads no such part)
+__device__ __forceinline__ void down_sums(const AdapterArgs& a, const Group& G, int n, int rank, int r0, int c_begin, int c_end,
+                                          float (&sum)[kDownThreads / 32][MT * 16 * kGroup]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const T* down = static_cast<const T*>(a.down) + (size_t)which * a.rank * a.cols;
+    const T* down = static_cast<const T*>(a.down) + (size_t)G.adapter * a.rank * a.cols;
     const float* x = g < n ? a.X + (long long)G.member[g] * a.ldx : a.X;
     float d[MT][4];
 #pragma unroll
     for (int m = 0; m < MT; ++m) d[m][0] = d[m][1] = d[m][2] = d[m][3] = 0.f;
-    const int c_end = min(a.cols, ((int)blockIdx.y + 1) * a.split_cols);
-    for (int c0 = (int)blockIdx.y * a.split_cols + warp * 32; c0 < c_end; c0 += kDownThreads) {
+    for (int c0 = c_begin + warp * 32; c0 < c_end; c0 += kDownThreads) {
         const int c = c0 + t * 8;
         float xv[8];
         uint32_t hi[8], lo[8];
@@ -231,37 +220,51 @@ __global__ void __launch_bounds__(kDownThreads) csb_adapter_down_kernel(AdapterA
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum[warp][(2 * t + (k & 1)) * MT * 16 + m * 16 + g + (k >> 1) * 8] = d[m][k];
+}
+template <int N>
+__device__ __forceinline__ float sum_of_warps(const float (&sum)[kDownThreads / 32][N], int i) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < kDownThreads / 32; ++w) s += sum[w][i];
+    return s;
+}
+
+// part[split][b][:] = down_a X[b, columns of the split].
+template <typename T, int MT, bool VEC>
+__global__ void __launch_bounds__(kDownThreads) csb_adapter_down_kernel(AdapterArgs a) {
+    __shared__ Group G;
+    __shared__ float sum[kDownThreads / 32][MT * 16 * kGroup];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int n = find_group<kDownThreads>(a, blockIdx.x, G);
+    if (blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < 2 + kGroup) {
+        const int i = threadIdx.x;
+        a.groups[blockIdx.x * kGroupWords + i] = i == 0 ? (n ? G.adapter : 0) : i == 1 ? n : i - 2 < n ? G.member[i - 2] : 0;
+    }
+    if (!n) return;
+    const int rank = rank_of(a, G.adapter), r0 = (int)blockIdx.z * MT * 16;
+    if (r0 >= rank) return;                                      // (the other kernel reads no such part)
+    const int c_begin = (int)blockIdx.y * a.split_cols;
+    down_sums<T, MT, VEC>(a, G, n, rank, r0, c_begin, min(a.cols, c_begin + a.split_cols), sum);
     __syncthreads();
     for (int i = threadIdx.x; i < MT * 16 * n; i += kDownThreads) {
         const int r = r0 + i % (MT * 16);
-        if (r >= a.rank_pad) continue;
-        float s = 0.f;
-#pragma unroll
-        for (int w = 0; w < kDownThreads / 32; ++w) s += sum[w][i];
-        a.part[((size_t)blockIdx.y * a.batch + G.member[i / (MT * 16)]) * a.rank_pad + r] = s;
+        if (r < a.rank_pad) a.part[((size_t)blockIdx.y * a.batch + G.member[i / (MT * 16)]) * a.rank_pad + r] = sum_of_warps(sum, i);
     }
 }
 
-// Y[b, rows] += s_a up_a (sum of the parts).  A warp takes 16 rows at a time, RT times 16 ranks at a time (all of them up to a
+// Y[member, rows of the CTA] += up_a low, where low(hi, lo) leaves s_a down_a X[member] as two halves.  A warp takes 16 rows at a time, RT times 16 ranks at a time (all of them up to a
 // rank of 64); lane 4g + t has ranks 4t .. 4t + 3 of every 16 of rows g and g + 8 (again two steps in an order of their own).
-// Bound by latency: what a tile needs is loaded a tile ahead, the first one's beside the parts.
-template <typename T, int RT, bool VEC>
-__global__ void __launch_bounds__(kUpThreads) csb_adapter_up_kernel(const AdapterArgs a, int rows_a_cta) {
-    __shared__ __align__(16) uint32_t hi[kGroup][kMaxRank + 16], lo[kGroup][kMaxRank + 16];
-    pdl_launch_dependents();
-    pdl_wait();
-    const int32_t* group = a.groups + blockIdx.x * kGroupWords;
-    const int which = group[0], n = group[1];
-    if (!n) return;
-    const int rank = rank_of(a, which);
-    if (rank == 0) return;
-    const float scale = a.scales ? a.scales[which] : 1.f;
+// Bound by latency: what a tile needs is loaded a tile ahead, the first one's beside low.
+template <typename T, int RT, bool VEC, int WIDTH, typename F>
+__device__ __forceinline__ void up_rows(const AdapterArgs& a, int which, const int32_t* member, int n, int rank, int rows_a_cta, F&& low) {
+    __shared__ __align__(16) uint32_t hi[kGroup][WIDTH + 16], lo[kGroup][WIDTH + 16];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const T* up = static_cast<const T*>(a.up) + (size_t)which * a.rank * a.rows;
     const int end = min(a.rows, ((int)blockIdx.y + 1) * rows_a_cta);
     const int j0 = min(2 * t, n - 1), j1 = min(2 * t + 1, n - 1);
-    float* y0 = a.Y + (long long)group[2 + j0] * a.ldy;
-    float* y1 = a.Y + (long long)group[2 + j1] * a.ldy;
+    float* y0 = a.Y + (long long)member[j0] * a.ldy;
+    float* y1 = a.Y + (long long)member[j1] * a.ldy;
     // (what is not there is read elsewhere in the tensors and dropped)
     float u[RT][2][4], y[4];
     auto load_up = [&](int i0, int r0) {
@@ -284,16 +287,7 @@ __global__ void __launch_bounds__(kUpThreads) csb_adapter_up_kernel(const Adapte
     };
     int i0 = (int)blockIdx.y * rows_a_cta + warp * 16;
     if (i0 < end) { load_up(i0, 0); load_y(i0); }
-    for (int i = threadIdx.x; i < kGroup * a.rank_pad; i += kUpThreads) {
-        const int j = i / a.rank_pad, r = i % a.rank_pad;
-        float s = 0.f;
-        if (j < n && r < rank) {
-            const float* p = a.part + (size_t)group[2 + j] * a.rank_pad + r;
-#pragma unroll 8
-            for (int k = 0; k < a.splits; ++k) s += p[(size_t)k * a.batch * a.rank_pad];
-        }
-        split_tf32(s * scale, hi[j][r], lo[j][r]);
-    }
+    low(hi, lo);
     __syncthreads();
     for (; i0 < end; i0 += kUpThreads / 2) {
         float d[4] = {0.f, 0.f, 0.f, 0.f};
@@ -335,6 +329,53 @@ __global__ void __launch_bounds__(kUpThreads) csb_adapter_up_kernel(const Adapte
             if (r1 < end) y1[r1] = old[3] + d[3];
         }
     }
+}
+
+// The parts' sums are the low-rank values.
+template <typename T, int RT, bool VEC>
+__global__ void __launch_bounds__(kUpThreads) csb_adapter_up_kernel(const AdapterArgs a, int rows_a_cta) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int32_t* group = a.groups + blockIdx.x * kGroupWords;
+    const int which = group[0], n = group[1];
+    if (!n) return;
+    const int rank = rank_of(a, which);
+    if (rank == 0) return;
+    const float scale = a.scales ? a.scales[which] : 1.f;
+    up_rows<T, RT, VEC, kMaxRank>(a, which, group + 2, n, rank, rows_a_cta, [&](auto& hi, auto& lo) {
+        for (int i = threadIdx.x; i < kGroup * a.rank_pad; i += kUpThreads) {
+            const int j = i / a.rank_pad, r = i % a.rank_pad;
+            float s = 0.f;
+            if (j < n && r < rank) {
+                const float* p = a.part + (size_t)group[2 + j] * a.rank_pad + r;
+#pragma unroll 8
+                for (int k = 0; k < a.splits; ++k) s += p[(size_t)k * a.batch * a.rank_pad];
+            }
+            split_tf32(s * scale, hi[j][r], lo[j][r]);
+        }
+    });
+}
+// Both in one launch: every CTA takes the low-rank values of its group for itself.
+template <typename T, int RT, bool VEC>
+__global__ void __launch_bounds__(kUpThreads) csb_adapter_kernel(const AdapterArgs a, int rows_a_cta) {
+    static_assert(kUpThreads == kDownThreads, "one CTA does both");
+    __shared__ Group G;
+    __shared__ float sum[kDownThreads / 32][RT * 16 * kGroup];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int n = find_group<kUpThreads>(a, blockIdx.x, G);
+    if (!n) return;
+    const int rank = rank_of(a, G.adapter);
+    if (rank == 0) return;
+    const float scale = a.scales ? a.scales[G.adapter] : 1.f;
+    up_rows<T, RT, VEC, RT * 16>(a, G.adapter, G.member, n, rank, rows_a_cta, [&](auto& hi, auto& lo) {
+        down_sums<T, RT, VEC>(a, G, n, rank, 0, 0, a.cols, sum);
+        __syncthreads();
+        for (int i = threadIdx.x; i < RT * 16 * kGroup; i += kUpThreads) {
+            const int j = i / (RT * 16), r = i % (RT * 16);
+            split_tf32(j < n && r < rank ? sum_of_warps(sum, i) * scale : 0.f, hi[j][r], lo[j][r]);
+        }
+    });
 }
 
 #define CSB_CUDA(call)                                                                     \
@@ -388,6 +429,13 @@ static cudaError_t launch_down(const AdapterArgs& a, unsigned groups, size_t sme
                                grid, kDownThreads, smem, stream, a);
 }
 
+// Whether every CTA of the second kernel may as well compute the low-rank values for itself: one launch less, against every CTA going
+// through the columns.  40 requests of 20 adapters on 2048 rows: rank 64 on 512 columns 21.8 us (with two kernels 26.6), rank 16 on 2048
+// columns 23.4 (25.3); 48 of 24 of rank 16 on 8192 x 4096 45 us (31).
+constexpr int64_t kOneKernel = 32768;
+constexpr int kOneCtas = 444;
+static bool one_kernel(const AdapterArgs& a) { return a.rank_pad <= 64 && (int64_t)a.rank_pad * a.cols <= kOneKernel; }
+
 template <typename T>
 static int adapters_on_device(const csb_matrix* A, AdapterArgs a, void* stream) {
     auto aligned = [](const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; };
@@ -396,19 +444,22 @@ static int adapters_on_device(const csb_matrix* A, AdapterArgs a, void* stream) 
     a.by_adapter = groups_by_adapter(a.batch, a.count);
     const unsigned groups = (unsigned)(a.by_adapter ? most_groups(a.batch, a.count) : a.batch);
     const size_t smem = a.by_adapter ? (size_t)a.count * 4 : 0;
-    CSB_CUDA((down_vec ? launch_down<T, true>(a, groups, smem, stream) : launch_down<T, false>(a, groups, smem, stream)));
+    const bool one = one_kernel(a);
+    if (!one) CSB_CUDA((down_vec ? launch_down<T, true>(a, groups, smem, stream) : launch_down<T, false>(a, groups, smem, stream)));
     const int rc = guarded([&] { return product_any(A, a.X, a.ldx, a.batch, a.Y, a.ldy, stream); });
     if (rc != CSB_OK) return rc;
     // rows of a CTA: a multiple of what it takes in one turn
+    const int tiles = a.rank_pad / 16;
     const int64_t turns = (a.rows + kUpThreads / 2 - 1) / (kUpThreads / 2);
-    const int64_t cuts = std::min<int64_t>(turns, std::max<int64_t>(1, wanted_up(a.rank_pad / 16) / most_groups(a.batch, a.count)));
+    const int64_t cuts = std::min<int64_t>(turns, std::max<int64_t>(1, (one ? kOneCtas : wanted_up(tiles)) / most_groups(a.batch, a.count)));
     const int rows = (int)((turns + cuts - 1) / cuts * (kUpThreads / 2));
     const dim3 grid(groups, (unsigned)((a.rows + rows - 1) / rows));
-    const int tiles = a.rank_pad / 16;
-    void (*up)(const AdapterArgs, int) =
-        up_vec ? (tiles == 1 ? csb_adapter_up_kernel<T, 1, true> : tiles == 2 ? csb_adapter_up_kernel<T, 2, true> : csb_adapter_up_kernel<T, 4, true>)
-               : (tiles == 1 ? csb_adapter_up_kernel<T, 1, false> : tiles == 2 ? csb_adapter_up_kernel<T, 2, false> : csb_adapter_up_kernel<T, 4, false>);
-    CSB_CUDA((launch<AdapterArgs, int>(up, grid, kUpThreads, 0, stream, a, rows)));
+    void (*up)(const AdapterArgs, int);
+    if (one && down_vec && up_vec) up = tiles == 1 ? csb_adapter_kernel<T, 1, true> : tiles == 2 ? csb_adapter_kernel<T, 2, true> : csb_adapter_kernel<T, 4, true>;
+    else if (one) up = tiles == 1 ? csb_adapter_kernel<T, 1, false> : tiles == 2 ? csb_adapter_kernel<T, 2, false> : csb_adapter_kernel<T, 4, false>;
+    else if (up_vec) up = tiles == 1 ? csb_adapter_up_kernel<T, 1, true> : tiles == 2 ? csb_adapter_up_kernel<T, 2, true> : csb_adapter_up_kernel<T, 4, true>;
+    else up = tiles == 1 ? csb_adapter_up_kernel<T, 1, false> : tiles == 2 ? csb_adapter_up_kernel<T, 2, false> : csb_adapter_up_kernel<T, 4, false>;
+    CSB_CUDA((launch<AdapterArgs, int>(up, grid, kUpThreads, one ? smem : 0, stream, a, rows)));
     return CSB_OK;
 }
 

@@ -52,7 +52,7 @@ def near(Y, W, X, down, up, which, ranks=None, scales=None):
 CASES = [  # rows, cols, batch, adapters, rank, matrix type
     (64, 48, 1, 1, 1, "f16"), (300, 177, 1, 2, 8, "f16"), (512, 192, 5, 3, 12, "f32"), (96, 256, 9, 4, 16, "f16"), (257, 640, 33, 2, 17, "f16"),
     (128, 129, 64, 40, 33, "f16"), (80, 520, 100, 3, 64, "f16"), (48, 64, 20, 2, 100, "f16"), (40, 300, 1100, 5, 9, "f16"), (1030, 72, 3, 1, 256, "f32"),
-    (64, 64, 1300, 1, 4, "f16"),
+    (64, 64, 1300, 1, 4, "f16"), (64, 2600, 30, 8, 16, "f16"), (72, 1111, 70, 3, 40, "f16"), (200, 1500, 2, 2, 64, "f32"),
 ]
 
 
