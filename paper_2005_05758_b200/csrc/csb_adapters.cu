@@ -199,7 +199,7 @@ __device__ __forceinline__ void down_sums(const AdapterArgs& a, const Group& G, 
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             const int r = r0 + m * 16 + g;
-            float u[8], v[8];
+            float u[8], v[8], e[4] = {0.f, 0.f, 0.f, 0.f};       // (the tensor cores cut their sums off; a turn's is added rounded)
             eight<VEC>(down + (size_t)min(r, rank - 1) * a.cols, c, c_end, r < rank, u);
             eight<VEC>(down + (size_t)min(r + 8, rank - 1) * a.cols, c, c_end, r + 8 < rank, v);
 #pragma unroll
@@ -209,11 +209,13 @@ __device__ __forceinline__ void down_sums(const AdapterArgs& a, const Group& G, 
                     uint32_t wl[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) split_tf32(__uint_as_float(w[k]), w[k], wl[k]);
-                    mma_tf32(d[m], wl, hi[i], hi[i + 1]);
+                    mma_tf32(e, wl, hi[i], hi[i + 1]);
                 }
-                mma_tf32(d[m], w, lo[i], lo[i + 1]);
-                mma_tf32(d[m], w, hi[i], hi[i + 1]);
+                mma_tf32(e, w, lo[i], lo[i + 1]);
+                mma_tf32(e, w, hi[i], hi[i + 1]);
             }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) d[m][k] += e[k];
         }
     }
 #pragma unroll
