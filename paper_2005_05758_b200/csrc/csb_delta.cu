@@ -228,7 +228,7 @@ static int recurrent_any(int dtype, const DeltaArgs& a, void* stream) {
 
 // Sequences of up to kShort tokens go token by token where that kernel is launched: a chunk takes as long.  The host does not know the
 // lengths: a call of up to kShort tokens has no longer sequence; where there are many sequences, or few tokens for each, both
-// kernels are launched and each takes its own (256 requests that decode beside a prompt of 1500 tokens, 32 heads: 338 us, in
+// kernels are launched and each takes its own (256 requests that decode beside a prompt of 1500 tokens, 32 heads: 333 us, in
 // chunks alone 992); else
 // chunks serve the few that may be short.
 constexpr int kShort = kLong - 1;
