@@ -8,7 +8,8 @@ of the library's functions fails loudly when the shared library is missing.
 it exists; everything else is loaded from ``binding`` on first use.
 """
 _LAZY = ("CsbError", "CsbMatrix", "lib", "csb_encode", "csb_spmv", "csb_spmm", "csb_lstm_forward",
-         "csb_gru_forward", "spmv", "spmm", "lstm_forward", "gru_forward")
+         "csb_gru_forward", "csb_spmm_adapters", "csb_gated_delta_forward", "csb_gated_delta_step",
+         "spmv", "spmm", "lstm_forward", "gru_forward")
 
 
 def __getattr__(name):

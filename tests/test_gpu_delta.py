@@ -175,6 +175,21 @@ def test_gates_at_their_ends(T, dtype):
     check(a, [T])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(64, 48), (128, 33), (200, 20)])
+def test_growth_in_some_chunks(dk, dv, dtype):
+    a = draw(20, 140, 1, 2, dk, dv, dtype, slots=1)
+    a["g"][[5, 40, 41, 90]] = 0.02                               # (the states grow by a few hundredths: no more than the tolerance is for)
+    a["beta"][100:] *= -0.1                                      # and writes that take away
+    check(a, [140])
+
+
+def test_a_long_memory():
+    a = draw(21, 2500, 1, 1, 128, 16, "f32", slots=1)
+    a["g"][:] = -1e-4
+    check(a, [2500])
+
+
 @pytest.mark.parametrize("T", [6, 150])
 def test_the_same_key_again_and_zero_keys(T):
     a = draw(11, T, 1, 2, 64, 32, "f32", slots=1)
