@@ -68,8 +68,8 @@ __global__ void __launch_bounds__(kDeltaMaxWarps * 32) csb_delta_recurrent_kerne
         }
     }
     const T *qp = static_cast<const T*>(a.q) + hk * a.k_dim, *kp = static_cast<const T*>(a.k) + hk * a.k_dim;
-    const T* vp = static_cast<const T*>(a.v) + h * a.v_dim;
-    T* op = static_cast<T*>(a.o) + h * a.v_dim;
+    const T* vp = static_cast<const T*>(a.v) + (long long)h * a.v_dim;
+    T* op = static_cast<T*>(a.o) + (long long)h * a.v_dim;
     for (long long t = t0; t < t1; ++t) {
         const int at = (int)((t - t0) & 1);
         for (int i = threadIdx.x; i < a.k_dim; i += blockDim.x) {

@@ -286,6 +286,15 @@ def test_states_past_32_bits_of_elements():
         near(pool[[n - 1, 3]].flatten(0, 1), want_S.reshape(-1, 128, 128), T, 128)
 
 
+def test_a_token_past_32_bits_of_elements():
+    H, dv = 40000, 65536
+    v, o = torch.zeros((1, H, dv), dtype=torch.float16, device="cuda"), torch.zeros((1, H, dv), dtype=torch.float16, device="cuda")
+    v[0, -1], v[0, 0, :5] = 2.0, 3.0
+    one, g = torch.ones((1, 1, 1), dtype=torch.float16, device="cuda"), torch.zeros((1, H), device="cuda")
+    binding.csb_gated_delta_forward(one, one, v, g, torch.full((1, H), 0.5, device="cuda"), o)
+    assert torch.all(o[0, -1] == 1.0) and torch.all(o[0, 0, :5] == 1.5) and torch.all(o[0, 0, 5:] == 0) and torch.all(o[0, -2] == 0)
+
+
 @pytest.mark.parametrize("lens", [[2, 3], [90, 33]])
 def test_bits_are_the_same_again_on_another_stream_and_in_a_graph(lens):
     begin = torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32, device="cuda")
